@@ -284,6 +284,133 @@ int kvmix_dequant(const kvmix_shape* shape, const kvmix_layer_cfg* cfg,
  * launch it gives the read rate a launch of that shape and size can reach on the machine at hand. */
 int kvmix_stream_read(const void* buf, size_t bytes, int workgroups, int threads, void* sink, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Paged cache: sequences of lengths of their own that come, fork and go.
+ *
+ * A page is one tile record of every kv head: pool is [n_pages][Hkv][record], the records of the layout statement above. A Key
+ * group runs along 32 tokens, so that a page is written once, whole, by the launch in which its 32 tokens leave the fp16 window,
+ * and never again: sequences that fork share pages without any copy of them.
+ * A sequence occupies a slot s of n_slots: row s of `table` (page ids of its tiles, oldest first), lens[s] and a ring of W_cap rows in
+ * both fp16 windows. Ageing is the fixed window's (kvmix_append), with everything a function of the length n:
+ *   packed tiles  P(n) = n < window + 32 ? 0 : (n - window) / 32,
+ *   token t >= 32 P(n) is row t % W_cap of the slot's rings.
+ * The state lives on the device, so that a decode loop can be captured into a graph: the integers of kvmix_pages (shared by all
+ * layers, which then have one window length) and a kvmix_paged_cache for each layer. A step is
+ *   kvmix_pages_grow(rows, cu)                                   once: lengths, pages for the tiles that fall due
+ *   kvmix_qk_norm_rope, kvmix_paged_append, kvmix_paged_decode_attn   for each layer
+ * `rows`: the slot of every batch row (NULL: row b is slot b); a negative one is padding, for which nothing is read or written. The
+ * slots of a batch are distinct where a call writes to them. `cu`: n_rows + 1 offsets, row b brings the tokens [cu[b], cu[b + 1]) of the
+ * call's inputs (NULL: token b alone).
+ * What the host cannot see is checked on the device: nothing is read or written outside the buffers whatever these integers
+ * say, and `status` (sticky, cleared by the caller) takes the bits of kvmix_page_status.
+ * Widths are 1 to 4 bits (a 16-bit layer has nothing to page: KVMIX_ERR_BAD_BITS), group sizes those of kvmix_decode_attn. */
+enum {                       /* bits of kvmix_pages.status */
+  KVMIX_PAGES_EXHAUSTED = 1, /* kvmix_pages_grow: too few free pages, or more tiles than a table row holds: the row keeps its length */
+  KVMIX_PAGES_BAD_ROW = 2,   /* a slot out of range, the same one twice, a length or an offset that cannot be */
+  KVMIX_PAGES_BAD_ID = 4,    /* a page id out of range in the table or in a list of copies */
+  KVMIX_PAGES_OCCUPIED = 8   /* kvmix_pages_fork: the destination holds tokens, or is a source or a destination of the same call already */
+};
+
+typedef struct {             /* every pointer: device memory, 4-byte aligned (moves: 16) */
+  int32_t* table;            /* [n_slots][max_tiles] page ids; entries past a sequence's tiles are not read */
+  int32_t* lens;             /* [n_slots] tokens, those of the step in hand among them once kvmix_pages_grow has run */
+  int32_t* grown;            /* [n_slots] tokens granted by the last kvmix_pages_grow (0 after a fork or free): what kvmix_paged_append takes */
+  int32_t* refs;             /* [n_pages] slots that hold the page */
+  uint32_t* used;            /* [(n_pages + 31) / 32] bit p % 32 of word p / 32: refs[p] > 0; bits past n_pages zero */
+  int32_t* status;           /* [1] */
+  int32_t* moves;            /* [4 + 3 * n_pages] of kvmix_pages_compact, may be NULL otherwise: count, pages in use, 2 unused; sources;
+                                destinations; scratch */
+  int32_t n_slots, n_pages;
+  int32_t max_tiles;         /* entries of a table row */
+  int32_t window;            /* kvmix_layer_cfg.window of every layer, >= 0 */
+} kvmix_pages;
+
+typedef struct {             /* one layer's buffers (device, 16-byte aligned) */
+  uint32_t* pool;            /* [n_pages][Hkv][record] */
+  uint16_t* k_win;           /* [n_slots][Hkv][W_cap][128] */
+  uint16_t* v_win;
+  int32_t n_pages, n_slots;  /* as in kvmix_pages */
+  int32_t W_cap;             /* multiple of 32, >= window + 32 */
+} kvmix_paged_cache;
+
+/* Rows grow by their tokens: lens[s] += cu[b + 1] - cu[b], grown[s] = that. The tiles that fall due get pages: the lowest free
+ * ids, in the order of the rows and of the tiles. Rows are granted in order while the free pages last (a row that needs none always is);
+ * one that is not keeps its length, has grown[s] = 0 and sets a status bit. At most 4096 rows; window + new tokens below 2^31. */
+int kvmix_pages_grow(const kvmix_pages* pages, const int32_t* rows, const int32_t* cu, int n_rows, void* stream);
+/* Slots are emptied: their pages' counts go down, pages that nobody holds are free. A slot named twice is freed once. */
+int kvmix_pages_free(const kvmix_pages* pages, const int32_t* rows, int n_rows, void* stream);
+/* Slot dst[i] (empty) becomes a second holder of the pages of slot src[i] and gets its length; the rings' rows are copied per layer by
+ * kvmix_copy_windows. One source may have many destinations; a pair whose destination holds tokens, is named twice or is a source
+ * of the same call is left out and sets a status bit. Negative slots: padding. At most 4096 pairs. */
+int kvmix_pages_fork(const kvmix_pages* pages, const int32_t* src, const int32_t* dst, int n_pairs, void* stream);
+/* Pages in use move to the ids [0, in use): the i-th highest-numbered in use past that end (in ascending order) to the i-th free id below
+ * it. Table, counts and bits are rewritten; moves holds the list for kvmix_move_records, which every layer's pool needs before it is
+ * next read or written. */
+int kvmix_pages_compact(const kvmix_pages* pages, void* stream);
+/* The records of the moves of the last kvmix_pages_compact, within the pool. Contents of freed pages are left as they are. */
+int kvmix_move_records(const kvmix_shape* shape, const kvmix_layer_cfg* cfg, const kvmix_paged_cache* cache,
+                       const kvmix_pages* pages, void* stream);
+/* Both rings of slot src[i] to slot dst[i], all W_cap rows. Destinations are distinct and none is a source; a pair with a negative
+ * slot is padding, one out of range is left out. At most 65535 pairs. */
+int kvmix_copy_windows(const kvmix_shape* shape, const kvmix_layer_cfg* cfg, const kvmix_paged_cache* cache,
+                       const int32_t* src, const int32_t* dst, int n_pairs, void* stream);
+
+/* kvmix_append_tokens for a ragged batch, after kvmix_pages_grow: the tokens [cu[b], cu[b + 1]) of k_new, v_new (element (i, j, d) of
+ * each at i*token_stride + j*head_stride + d; strides of their own, in elements, multiples of 8, not negative; 16-byte aligned) are the newest of
+ * slot rows[b], b < shape->B. Tiles that fall due are quantized into their pages exactly as in kvmix_quantize_pack, from the ring or
+ * straight from the input; what stays goes into the ring; one launch. max_new: no row brings more tokens (the grid's size). A
+ * row whose token count is not what grown[s] says, or exceeds max_new, is left alone. */
+int kvmix_paged_append(const kvmix_shape* shape, const kvmix_layer_cfg* cfg,
+                       const uint16_t* k_new, int64_t k_token_stride, int64_t k_head_stride,
+                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride,
+                       const kvmix_paged_cache* cache, const kvmix_pages* pages,
+                       const int32_t* rows, const int32_t* cu, int max_new, void* stream);
+
+/* Workspace of kvmix_paged_decode_attn for lengths up to max_len: zero-filled once, for one shape and max_len; calls that overlap in time
+ * need one each. */
+int kvmix_paged_workspace_bytes(const kvmix_shape* shape, int max_len, size_t* bytes);
+/* kvmix_decode_attn for a ragged batch: q, out fp16 [shape->B][Hq][128], row b attends to the lens[s] tokens of slot s = rows[b]. A
+ * sequence without tokens gives zeros; a padding row of out is left as it was; a length above max_len (<= 0: what a table row
+ * holds) or a page id out of range gives NaN. Contexts are split over workgroups in shares of equal size and joined in the same launch. */
+int kvmix_paged_decode_attn(const kvmix_shape* shape, const kvmix_layer_cfg* cfg, const uint16_t* q,
+                            const kvmix_paged_cache* cache, const kvmix_pages* pages, const int32_t* rows, int max_len,
+                            float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Between the projections and the cache. */
+typedef enum { KVMIX_F16 = 0, KVMIX_BF16 = 1, KVMIX_F32 = 2 } kvmix_dtype;
+typedef enum {
+  KVMIX_ROPE_PLAIN = 0,      /* f_i = base^(-2i / rotary_dim) radians per position */
+  KVMIX_ROPE_LINEAR = 1,     /* f_i / factor */
+  KVMIX_ROPE_BASE = 2,       /* base * factor^(rotary_dim / (rotary_dim - 2)): the fastest pair as it was, the slowest f / factor */
+  KVMIX_ROPE_TURNS = 3,      /* by the turns a pair makes in original_len positions: from `high` on f_i, up to `low` f_i / factor, linear between */
+  KVMIX_ROPE_INDEX = 4       /* the same ends, linear in the pair's index between the (real) indices that make `high` and `low` turns; amplitude
+                                0.1 ln(factor) + 1 */
+} kvmix_rope_scaling;
+/* Frequencies of the rotary_dim / 2 pairs (host memory, fp32; computed in binary64) and the factor for cosine and sine (may be NULL). Host
+ * arithmetic only. rotary_dim even, 2 to 128; base > 1; factor >= 1; original_len >= 1, 0 < low < high where the scaling has them. */
+int kvmix_rope_frequencies(int rotary_dim, double base, int scaling, double factor, int original_len, double low, double high,
+                           float* frequencies, float* amplitude);
+
+typedef struct {
+  const float* frequencies;  /* device, [rotary_dim / 2]: radians per position (NULL with rotary_dim 0) */
+  int32_t rotary_dim;        /* channels 0 .. rotary_dim - 1 of a head are rotated: a multiple of 16, 0 to 128 */
+  int32_t interleaved;       /* pairs (2i, 2i + 1); 0: (i, i + rotary_dim / 2) */
+  float amplitude;           /* of cosine and sine */
+  float eps;                 /* of the norms */
+  const void* q_weight;      /* device, [128] of the inputs' type, 16-byte aligned: x / sqrt(mean(x^2) + eps) * weight over the 128 channels ahead */
+  const void* k_weight;      /* of the rotation; NULL: no norm for that side */
+} kvmix_rope;
+/* Queries and Keys of n_tokens tokens as the projections leave them, normed and rotated by positions[i], and Values, as the fp16 that the cache
+ * and the attention take: out[i][head][128] for q (Hq heads), k, v (Hkv heads), contiguous. Inputs of one type (kvmix_dtype), element
+ * (i, h, d) of each at i*token_stride + h*head_stride + d with strides of their own (elements; multiples of 16 bytes; any sign or zero);
+ * pointers 16-byte aligned. Any of the three may be left out (input and output NULL). Angles are taken in binary64, everything else in
+ * fp32 with one rounding at the end; positions are any int32. Outputs may be the inputs' memory only where the layout is the same, element for
+ * element. One launch. */
+int kvmix_qk_norm_rope(const kvmix_shape* shape, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions,
+                       const void* q, int64_t q_token_stride, int64_t q_head_stride, uint16_t* q_out,
+                       const void* k, int64_t k_token_stride, int64_t k_head_stride, uint16_t* k_out,
+                       const void* v, int64_t v_token_stride, int64_t v_head_stride, uint16_t* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -72,6 +72,14 @@ def lib():
         L.kvmix_rpc_next.argtypes = [C.c_double, C.c_double, I, I, P, P]
         L.kvmix_flush.restype = I
         L.kvmix_flush.argtypes = [P, P, P, I, I, P]
+        for name, args in (("kvmix_pages_grow", [P, P, P, I, P]), ("kvmix_pages_free", [P, P, I, P]), ("kvmix_pages_fork", [P, P, P, I, P]),
+                           ("kvmix_pages_compact", [P, P]), ("kvmix_move_records", [P] * 5), ("kvmix_copy_windows", [P] * 5 + [I, P]),
+                           ("kvmix_paged_append", [P, P] + [P, I64, I64] * 2 + [P] * 4 + [I, P]), ("kvmix_paged_workspace_bytes", [P, I, P]),
+                           ("kvmix_paged_decode_attn", [P] * 6 + [I, C.c_float, P, P, SZ, P]),
+                           ("kvmix_rope_frequencies", [I, C.c_double, I, C.c_double, I, C.c_double, C.c_double, P, P]),
+                           ("kvmix_qk_norm_rope", [P, P, I, I, P] + [P, I64, I64, P] * 3 + [P])):
+            getattr(L, name).restype = I
+            getattr(L, name).argtypes = args
         L.kvmix_dequant.restype = I
         L.kvmix_dequant.argtypes = [P, P, P, I, P, P]
         _lib = L
@@ -238,3 +246,174 @@ def dequant(shape, cfg, cache, which, out):
     """out: fp32 CUDA tensor [units][n_q (Keys) or n_q + v_lead (Values)][128]."""
     _check(lib().kvmix_dequant(C.byref(shape), C.byref(cfg), C.byref(cache.c), which, out.data_ptr(), _stream()), "kvmix_dequant")
     return out
+
+
+# ---- the paged cache
+class _PagesStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "lens", "grown", "refs", "used", "status", "moves")] + \
+               [(n, C.c_int32) for n in ("n_slots", "n_pages", "max_tiles", "window")]
+
+
+class _PagedCacheStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pool", "k_win", "v_win")] + [(n, C.c_int32) for n in ("n_pages", "n_slots", "W_cap")]
+
+
+class _RopeStruct(C.Structure):
+    _fields_ = [("frequencies", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float), ("eps", C.c_float),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+def _int32(t, n, what):
+    """Device address of a contiguous int32 tensor of at least n elements (n None: any); None stays None."""
+    if t is None:
+        return None
+    assert t.element_size() == 4 and not t.is_floating_point() and t.is_contiguous(), f"{what}: contiguous int32 expected"
+    assert n is None or t.numel() >= n, f"{what}: {t.numel()} elements, {n} expected"
+    return t.data_ptr()
+
+
+class Pages:
+    """Which sequence holds which pages, for all layers: int32 tensors table [n_slots][max_tiles], lens, grown [n_slots], refs [n_pages],
+    used [(n_pages + 31) // 32], status [1], moves [4 + 3 n_pages]. buffers: some of them, where the caller has them already (the others
+    are made, empty; `moves` only when pages_compact is first called)."""
+
+    def __init__(self, n_slots, n_pages, max_tiles, window, device="cuda", buffers=None):
+        import torch
+        sizes = dict(table=n_slots * max_tiles, lens=n_slots, grown=n_slots, refs=n_pages, used=(n_pages + 31) // 32, status=1)
+        shapes = dict(table=(n_slots, max_tiles))
+        self.n_slots, self.n_pages, self.max_tiles, self.window, self.device = n_slots, n_pages, max_tiles, window, device
+        given = dict(buffers or {})
+        for name, n in sizes.items():
+            t = given.pop(name, None)
+            if t is None:
+                t = torch.zeros(shapes.get(name, (n,)), dtype=torch.int32, device=device)
+            setattr(self, name, t)
+        self.moves = given.pop("moves", None)
+        assert not given, f"unknown buffers {sorted(given)}"
+        self.c = _PagesStruct(*[_int32(getattr(self, name), n, name) for name, n in sizes.items()], _int32(self.moves, 4 + 3 * n_pages, "moves"),
+                              n_slots, n_pages, max_tiles, window)
+
+    def _with_moves(self):
+        if self.moves is None:
+            import torch
+            self.moves = torch.zeros(4 + 3 * self.n_pages, dtype=torch.int32, device=self.device)
+            self.c.moves = self.moves.data_ptr()
+        return C.byref(self.c)
+
+
+class PagedCache:
+    """One layer of a paged cache: pool int32 [n_pages][Hkv][record words], k_win and v_win fp16 [n_slots][Hkv][W_cap][128]. buffers: as for
+    Pages (a layer whose rings alone, or whose pool alone, a call touches may have the rest left out: buffers names those that are there)."""
+
+    def __init__(self, shape, cfg, n_pages, n_slots, W_cap, device="cuda", buffers=None):
+        import torch
+        words = cache_bytes(shape, cfg, 32, max(W_cap, 32))["packed"] // (4 * shape.units)
+        made = dict(pool=lambda: torch.zeros((n_pages, shape.Hkv, words), dtype=torch.int32, device=device),
+                    k_win=lambda: torch.zeros((n_slots, shape.Hkv, W_cap, 128), dtype=torch.float16, device=device))
+        made["v_win"] = made["k_win"]
+        sizes = dict(pool=n_pages * shape.Hkv * words * 4, k_win=n_slots * shape.Hkv * W_cap * 256, v_win=n_slots * shape.Hkv * W_cap * 256)
+        for name, make in made.items():
+            t = make() if buffers is None else buffers.get(name)
+            assert t is None or (t.is_contiguous() and t.numel() * t.element_size() >= sizes[name]), f"{name}: {sizes[name]} contiguous bytes expected"
+            setattr(self, name, t)
+        self.n_pages, self.n_slots, self.W_cap = n_pages, n_slots, W_cap
+        self.c = _PagedCacheStruct(*[None if t is None else t.data_ptr() for t in (self.pool, self.k_win, self.v_win)], n_pages, n_slots, W_cap)
+
+
+def pages_grow(pages, rows=None, cu=None, n_rows=None, stream=None):
+    """Rows (slots; None: row b is slot b) get room for cu[b + 1] - cu[b] more tokens each (None: one)."""
+    n = n_rows if n_rows is not None else rows.numel() if rows is not None else cu.numel() - 1
+    _check(lib().kvmix_pages_grow(C.byref(pages.c), _int32(rows, n, "rows"), _int32(cu, n + 1, "cu"), n, _stream(stream)), "kvmix_pages_grow")
+
+
+def pages_free(pages, rows, stream=None):
+    """The slots in `rows` are empty again, pages that nobody else holds are free."""
+    _check(lib().kvmix_pages_free(C.byref(pages.c), _int32(rows, None, "rows"), rows.numel(), _stream(stream)), "kvmix_pages_free")
+
+
+def pages_fork(pages, src, dst, stream=None):
+    """Slot dst[i], empty, becomes a second holder of the pages of src[i] (rings: copy_windows, per layer)."""
+    n = src.numel()
+    _check(lib().kvmix_pages_fork(C.byref(pages.c), _int32(src, n, "src"), _int32(dst, n, "dst"), n, _stream(stream)), "kvmix_pages_fork")
+
+
+def pages_compact(pages, stream=None):
+    """Pages in use move to the lowest ids; every layer's records follow by move_records."""
+    _check(lib().kvmix_pages_compact(pages._with_moves(), _stream(stream)), "kvmix_pages_compact")
+
+
+def move_records(shape, cfg, cache, pages, stream=None):
+    """One layer's records after pages_compact."""
+    _check(lib().kvmix_move_records(C.byref(shape), C.byref(cfg), C.byref(cache.c), C.byref(pages.c), _stream(stream)), "kvmix_move_records")
+
+
+def copy_windows(shape, cfg, cache, src, dst, stream=None):
+    """Both fp16 rings of slot src[i] to slot dst[i]."""
+    n = src.numel()
+    st = lib().kvmix_copy_windows(C.byref(shape), C.byref(cfg), C.byref(cache.c), _int32(src, n, "src"), _int32(dst, n, "dst"), n, _stream(stream))
+    _check(st, "kvmix_copy_windows")
+
+
+def paged_append(shape, cfg, k_new, v_new, cache, pages, rows=None, cu=None, max_new=1, stream=None):
+    """k_new, v_new: fp16 CUDA tensors [tokens][Hkv][128] (last dim contiguous, any strides otherwise), the tokens [cu[b], cu[b + 1]) of batch row b, at most max_new
+    each (cu None: token b), for which pages_grow has made room."""
+    ks, vs = k_new.stride(), v_new.stride()
+    assert k_new.element_size() == v_new.element_size() == 2 and ks[2] == vs[2] == 1 and k_new.shape == v_new.shape
+    st = lib().kvmix_paged_append(C.byref(shape), C.byref(cfg), k_new.data_ptr(), ks[0], ks[1], v_new.data_ptr(), vs[0], vs[1], C.byref(cache.c),
+                                  C.byref(pages.c), _int32(rows, shape.B, "rows"), _int32(cu, shape.B + 1, "cu"), max_new, _stream(stream))
+    _check(st, "kvmix_paged_append")
+
+
+def paged_workspace_bytes(shape, max_len):
+    n = C.c_size_t(0)
+    _check(lib().kvmix_paged_workspace_bytes(C.byref(shape), max_len, C.byref(n)), "kvmix_paged_workspace_bytes")
+    return n.value
+
+
+def paged_decode_attn(shape, cfg, q, cache, pages, out, workspace=None, rows=None, max_len=0, softmax_scale=0.0, stream=None):
+    """q, out: fp16 CUDA tensors [B][Hq][128], contiguous; row b attends to slot rows[b]'s tokens, max_len at most (0: what a table row holds).
+    workspace: uint8 CUDA tensor of paged_workspace_bytes, zeroed once."""
+    assert q.is_contiguous() and out.is_contiguous()
+    wp, wn = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+    st = lib().kvmix_paged_decode_attn(C.byref(shape), C.byref(cfg), q.data_ptr(), C.byref(cache.c), C.byref(pages.c), _int32(rows, shape.B, "rows"),
+                                       max_len, C.c_float(softmax_scale), out.data_ptr(), wp, wn, _stream(stream))
+    _check(st, "kvmix_paged_decode_attn")
+    return out
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
+
+
+def rope_frequencies(rotary_dim, base=10000.0, scaling="plain", factor=1.0, original_len=0, low=1.0, high=32.0):
+    """-> (rotary_dim // 2 floats: radians per position of each pair, factor for cosine and sine). Scalings: include/kvmix.h."""
+    out, amplitude = (C.c_float * 64)(), C.c_float(0.0)
+    _check(lib().kvmix_rope_frequencies(rotary_dim, base, ROPE_SCALINGS.get(scaling, -1), factor, original_len, low, high, out, C.byref(amplitude)),
+           "kvmix_rope_frequencies")
+    return list(out[:rotary_dim // 2]), amplitude.value
+
+
+def qk_norm_rope(shape, q, k, positions, frequencies, q_out, k_out, v=None, v_out=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                 amplitude=1.0, stream=None):
+    """q [tokens][Hq][128], k, v [tokens][Hkv][128]: fp16, bf16 or fp32 CUDA tensors of one type (last dim contiguous, any strides otherwise);
+    outputs fp16, contiguous. Heads are normed where a weight [128] is given, and the first 2 * len(frequencies) channels rotated (frequencies
+    None: none); v is converted only. Any of q, k, v may be None."""
+    import torch
+    some = [x for x in (q, k, v) if x is not None]
+    if not some:
+        return
+    n, dtype = some[0].shape[0], some[0].dtype
+    code = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}.get(dtype, -1)
+    sides = []
+    for x, o, heads in ((q, q_out, shape.Hq), (k, k_out, shape.Hkv), (v, v_out, shape.Hkv)):
+        if x is None:
+            sides += [None, 0, 0, None]
+            continue
+        assert x.dtype == dtype and tuple(x.shape) == (n, heads, 128) and x.stride(2) == 1
+        assert o.dtype == torch.float16 and o.shape == x.shape and o.is_contiguous()
+        sides += [x.data_ptr(), x.stride(0), x.stride(1), o.data_ptr()]
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == dtype and w.numel() == 128 and w.is_contiguous())
+    assert frequencies is None or (frequencies.dtype == torch.float32 and frequencies.is_contiguous())
+    rope = _RopeStruct(None if frequencies is None else frequencies.data_ptr(), 0 if frequencies is None else 2 * frequencies.numel(), int(interleaved),
+                       amplitude, eps, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
+    _check(lib().kvmix_qk_norm_rope(C.byref(shape), C.byref(rope), code, n, _int32(positions, n, "positions"), *sides, _stream(stream)), "kvmix_qk_norm_rope")

@@ -19,10 +19,14 @@ ATTN = ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"]
 # with 8 and with 12 waves per workgroup, each without and with the tiles between a Key front and a Value front
 OBJECTS = {
     "kvmix_quant.o": ("kvmix_quant.hip", ["-ffp-contract=off"]),
-    "kvmix_attn8.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=8", "-DKVMIX_MIXED=0"]),
-    "kvmix_attn12.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=0"]),
-    "kvmix_attn12_fronts.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=1"]),
+    "kvmix_attn8.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=8", "-DKVMIX_MIXED=0", "-DKVMIX_PAGED=0"]),
+    "kvmix_attn12.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=0", "-DKVMIX_PAGED=0"]),
+    "kvmix_attn12_fronts.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=1", "-DKVMIX_PAGED=0"]),
+    "kvmix_attn8_paged.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=8", "-DKVMIX_MIXED=0", "-DKVMIX_PAGED=1"]),
+    "kvmix_pages.o": ("kvmix_pages.hip", []),
+    "kvmix_rope.o": ("kvmix_rope.hip", []),
     "kvmix_api.o": ("kvmix_api.hip", []),
+    "kvmix_paged_api.o": ("kvmix_paged_api.hip", []),
 }
 
 

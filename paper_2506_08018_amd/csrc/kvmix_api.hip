@@ -26,14 +26,14 @@ int num_cus() {
   return n;
 }
 
-int hip_fail(hipError_t e) {
+}  // namespace
+
+int kvmix::hip_fail(hipError_t e) {
   g_last_hip_error.store((int)e);
   return KVMIX_ERR_HIP;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int check_shape_cfg(const kvmix_shape* sh, const kvmix_layer_cfg* cfg) {
+int kvmix::check_shape_cfg(const kvmix_shape* sh, const kvmix_layer_cfg* cfg) {
   if (!sh || !cfg) return KVMIX_ERR_NULL;
   if (sh->group != kTile) return KVMIX_ERR_BAD_GROUP;
   if (sh->D != kD || sh->B < 1 || sh->Hkv < 1 || sh->Hq < 1 || sh->Hq % sh->Hkv) return KVMIX_ERR_BAD_SHAPE;
@@ -49,6 +49,8 @@ int check_shape_cfg(const kvmix_shape* sh, const kvmix_layer_cfg* cfg) {
   if (cfg->window != -1 && (cfg->window < 0 || cfg->window % kTile)) return KVMIX_ERR_BAD_SHAPE;
   return KVMIX_OK;
 }
+
+namespace {
 
 // ring slot of token t (both windows)
 int slot_of(const kvmix_layer_cache* c, long long t) {

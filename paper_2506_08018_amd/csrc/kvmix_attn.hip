@@ -38,6 +38,7 @@ namespace {
 // 12 waves, one workgroup per CU: 168 registers per lane. 8 waves: 128 registers, two workgroups per CU.
 constexpr int kNW = KVMIX_WAVES;
 constexpr bool kMixed = KVMIX_MIXED;     // with tiles between a Key front and a Value front
+constexpr int kWindowTiles = 3;          // packed tiles that take a wave as long as one window tile (PAGED)
 constexpr int kMergeBatch = 32;          // splits whose partials the merging workgroup requests together (one round trip)
 // Reference of the running softmax (log2 units): numerators 2^(score - reference) are kept at or below 2^kRefCap;
 // when a score would exceed that, the reference is raised to (that score - kRefCap + 4), which leaves room for
@@ -399,9 +400,16 @@ template <int G, int NW> struct MergeLds {        // per-wave reference maximum 
 // memory, three reads in a row as the code comes to them, they kept the first requests back: 24 units x 4 heads, 6 splits 7.28 ->
 // 6.97 us per launch, 8 units x 8 heads x 2000 tokens 7.35 -> 6.99, 32 units x 1 head, 3 splits 6.06 -> 5.90; all read together at
 // the start 7.24, 7.20, 6.11. Few parameters: each costs the host's launch some 15 ns.
-template <int KB, int VB, int G, int NW, bool MIXED>
+//
+// PAGED: a ragged batch over pages (grid: kv heads and head blocks, batch rows, splits). What the host works out for a batch of one
+// length is worked out here from the sequence's: a split is a share of 2^chunk_log2 tiles of a context, window tiles counted
+// kWindowTiles each and taken by the last one, so that a workgroup knows its first page ids before it knows the length. (Equal shares
+// of each context instead would put the length's way from memory in front of the page ids'.) The shares that a sequence does not have end at once;
+// as the slowest dimension of the grid they are dispatched behind the ones that work. The preloaded words: pointers to the
+// batch's slots, lengths and page table, entries of its rows, the share and the kv heads.
+template <int KB, int VB, int G, int NW, bool MIXED, bool PAGED>
 __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kernel(
-    const uint16_t* q, const uint32_t* packed, u32x4_t shares, u32x4_t items, u32x2_t heads, AttnArgs a) {
+    const uint16_t* q, const uint32_t* packed, u32x4_t shares, u32x4_t items, u32x2_t heads, std::conditional_t<PAGED, PagedAttnArgs, AttnArgs> a) {
   constexpr int kWaves = NW;
   constexpr int kThreads = kWaves * kWave;
   // per wave: the exchange area of the packed tiles; before that, the staging area in which a window tile's
@@ -415,8 +423,11 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   __shared__ int s_done;   // waves that have delivered their result
 
   a.q = q; a.packed = packed;
+  if constexpr (PAGED) a.new_slot = -1;
+  else {
   a.n_splits = (int)shares[0]; a.win_each = (int)shares[1]; a.win_extra = (int)shares[2]; a.win_tiles = (int)shares[3];
   a.items_q = (int)items[0]; a.items_r = (int)items[1]; a.tiles_cap = (int)items[2]; a.n_w = (int)items[3];
+  }
   a.G = (int)heads[0]; a.head_blocks = (int)heads[1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // said to be uniform: what depends on it alone lives in scalar registers
@@ -424,13 +435,21 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   const int h = col & (G - 1);                       // head of the column (columns past the used ones repeat them)
   const bool lo_part = !kWide<G> && col >= 8;
   const bool col_valid = (col & 7) < G;              // the column's results are stored
-  const int sp = blockIdx.x, u = blockIdx.y;
+  int blk = (int)blockIdx.z, jh = 0;       // block of heads; kv head (PAGED)
+  if constexpr (PAGED) {
+    jh = (int)blockIdx.x; blk = 0;
+    if (a.head_blocks > 1) { jh = (int)blockIdx.x / a.head_blocks; blk = (int)blockIdx.x - jh * a.head_blocks; }
+  }
+  const int sp = PAGED ? blockIdx.z : blockIdx.x;
+  int u = blockIdx.y;
+  const int n_kv = PAGED ? (int)(items[3] >> 8) : 0;
+  if constexpr (PAGED) u = (int)blockIdx.y * n_kv + jh;
   // Query groups of more than 8 heads run as blocks of 8 or 16 heads in workgroups of their own (grid z): the blocks
   // of a unit read the same records and window rows at about the same time, so a tile comes from HBM once and from
   // the caches after that. uo numbers the (unit, head block) pairs; blocks of 8: rows uo*8 .. uo*8+7 of q and out.
   // Blocks of 16: the last one of a group may be partly empty; its idle columns repeat the group's last head.
-  const int uo = u * a.head_blocks + (int)blockIdx.z;
-  const int head0 = kWide<G> ? (int)blockIdx.z * G : 0;              // first head of the block inside the unit's group
+  const int uo = u * a.head_blocks + blk;
+  const int head0 = kWide<G> ? blk * G : 0;              // first head of the block inside the unit's group
   const int n_heads = kWide<G> ? (a.G - head0 < G ? a.G - head0 : G) : G;
   WaveLds<G>& L = s_wave[wave].x;
   uint16_t (&T)[kTile][kD] = s_wave[wave].t;
@@ -442,9 +461,25 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   // the others and a.win_tiles packed tiles less. (Quotient and remainder come from the host: the start of a launch is
   // latency-bound and integer division takes hundreds of instructions here.)
   const int extra = sp < a.win_extra ? sp : a.win_extra;
-  const int p_begin = sp * a.items_q + (sp < a.items_r ? sp : a.items_r) - extra * a.win_tiles;
-  const int p_end = p_begin + a.items_q + (sp < a.items_r ? 1 : 0) - (sp < a.win_extra ? a.win_tiles : 0);
-  const int n_win = a.win_each + (sp < a.win_extra ? 1 : 0);
+  int first = sp * a.items_q + (sp < a.items_r ? sp : a.items_r) - extra * a.win_tiles;
+  int last = first + a.items_q + (sp < a.items_r ? 1 : 0) - (sp < a.win_extra ? a.win_tiles : 0);
+  int wins = a.win_each + (sp < a.win_extra ? 1 : 0);
+  // PAGED: the slot and, as soon as it is known, the length and the page ids of the share's first 64 tiles (a lane each)
+  int slot = 0, n_tok = 0, ids = 0, ids_at = 0;
+  const int32_t* id_row = nullptr;
+  int n_ids = 0;                        // entries of a table row
+  bool spoiled = false;                 // nothing that could be trusted: the results are NaN
+  auto word_ptr = [](uint32_t lo, uint32_t hi) { return reinterpret_cast<const int32_t*>((uint64_t)hi << 32 | lo); };
+  auto load_ids = [&](int from) {      // page ids of the tiles from `from` on (a lane each, those within the table's row)
+    const int i = from + lane;
+    return i < n_ids ? id_row[i] : 0;
+  };
+  if constexpr (PAGED) {
+    const int32_t* rows = word_ptr(shares[0], shares[1]);
+    slot = rows ? load_uniform(rows + blockIdx.y) : (int)blockIdx.y;
+    n_ids = (int)items[2];
+    first = sp << (items[3] & 255u);
+  }
 
   // ---- the query and the wave's first tile are requested before anything else is done.
   // Packed tiles are claimed from a workgroup counter; the first claims are static (wave order).
@@ -456,7 +491,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   // loaded by the hi columns in use only (a load's cost at the start of a launch is its active lanes), copied to the lo columns later;
   // groups of 1 or 2 heads use it for window tiles only, and the other waves' requests are better spent on their first tiles (16 layers of
   // 256 units: 356.4 us with, 352.9 us without)
-  const bool needs_q = MIXED || G > 2 || wave < a.win_each + (sp < a.win_extra ? 1 : 0);
+  const bool needs_q = MIXED || PAGED || G > 2 || wave < a.win_each + (sp < a.win_extra ? 1 : 0);
 #pragma unroll
   for (int ks = 0; ks < 4; ks++) {
     qB[ks] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
@@ -476,7 +511,66 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   for (int hh = 0; hh < G; hh++) qraw[hh] = kOwnOperand<G> || kLateQuery ? 0u : reinterpret_cast<const uint32_t*>(qbase + hh * kD)[lane];
 
   constexpr uint32_t kRecBytes = (uint32_t)(record_words(KB, VB) * 4);
+  if constexpr (PAGED) {
+    if ((uint32_t)slot >= (uint32_t)a.n_slots) return;             // padding
+    id_row = word_ptr(items[0], items[1]) + (size_t)slot * n_ids;
+    n_tok = load_uniform(word_ptr(shares[2], shares[3]) + slot);
+    ids = load_ids(first);
+    ids_at = first;
+    int tiles = n_tok > 0 ? packed_tiles(n_tok, a.window) : 0;
+    a.n_w = n_tok - tiles * kTile;
+    wins = (a.n_w + kTile - 1) / kTile;
+    const int log2 = (int)(items[3] & 255u), share = 1 << log2, win_share = kWindowTiles * wins < share ? kWindowTiles * wins : share;
+    a.n_splits = (tiles + win_share + share - 1) >> log2;
+    if (a.n_splits < 1) a.n_splits = 1;
+    if (n_tok < 0 || n_tok > a.max_len || tiles > n_ids || a.n_splits > a.max_splits) { spoiled = true; tiles = 0; a.n_w = 0; wins = 0; a.n_splits = 1; }
+    if (sp >= a.n_splits) return;
+    if (sp < a.n_splits - 1) wins = 0;
+    a.w0_tile = ring_tile(tiles, a.ring_tiles, a.ring_magic);
+    last = first + share < tiles ? first + share : tiles;
+    if (first > last) first = last;
+  }
+  int n_pages = 0;
+  if constexpr (PAGED) n_pages = a.n_pages;
+  // (lanes past the share's tiles count for nothing)
+  auto check_ids = [&](int& x) {
+    const bool bad = (uint32_t)x >= (uint32_t)n_pages;
+    spoiled |= __any(bad && ids_at + lane < last) != 0;
+    x = bad ? 0 : x;
+  };
+  // (4 heads with 3-bit Keys and 3- or 4-bit Values have no register for the ids around the loop: in LDS, a copy for each wave)
+  constexpr bool kIdsInLds = PAGED && G == 4 && KB == 3 && VB >= 3;
+  __shared__ int s_ids[kIdsInLds ? kWaves : 1][kIdsInLds ? kWave : 1];
+  auto keep_ids = [&]() {
+    check_ids(ids);
+    if constexpr (kIdsInLds) {
+      int ln = lane;
+      asm volatile("" : "+v"(ln));       // (the address is not kept for the next time)
+      s_ids[wave][ln] = ids;
+      wave_lds_fence();
+    }
+  };
+  if constexpr (PAGED) keep_ids();
+  const int p_begin = first, p_end = last, n_win = wins;
+  const int uw = PAGED ? slot * n_kv + jh : u;                     // of the rings
   const rsrc_t up = make_rsrc(reinterpret_cast<const char*>(a.packed) + (size_t)u * a.tiles_cap * kRecBytes, (uint32_t)a.tiles_cap * kRecBytes);
+  // tile t (wave-uniform, the wave's tiles come in ascending order), past the end the last one
+  auto load_tile = [&](Stage<KB, VB>& st, int t, uint32_t l16) {
+    if constexpr (PAGED) {
+      if (t >= p_end) t = p_end - 1;
+      if (t - ids_at >= kWave) {       // (only shares of more than 64 tiles: contexts past 2 M tokens)
+        ids_at = t;
+        ids = load_ids(t);
+        keep_ids();
+      }
+      int id;
+      if constexpr (kIdsInLds) id = __builtin_amdgcn_readfirstlane(s_ids[wave][t - ids_at]);
+      else id = __builtin_amdgcn_readlane(ids, t - ids_at);
+      st.load(make_rsrc(reinterpret_cast<const char*>(a.packed) + ((size_t)(uint32_t)id * (uint32_t)n_kv + (uint32_t)jh) * kRecBytes, kRecBytes), 0, l16);
+    } else {
+      st.load(up, t < p_end ? t : p_end - 1, l16);
+    }
+  };
   const int n_early = n_win < kWaves ? kWaves - n_win : 0;      // waves n_win .. kWaves-1 start on packed tiles
   const bool has_packed = p_end > p_begin;
   const bool early = wave >= n_win;
@@ -503,7 +597,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   // live: tokens of the tile (from its first row on) that are there, at least one; has_new: the new token is the last of them
   auto win_load_k = [&](int slot0, int live, bool has_new, int lane, WinKeys& w) {
     const int col = lane & 15, kq = lane >> 4;
-    const uint16_t* kw = a.k_win + ((size_t)u * a.W_cap + slot0) * kD;
+    const uint16_t* kw = a.k_win + ((size_t)uw * a.W_cap + slot0) * kD;
     const uint16_t* kn = a.k_new + (size_t)u * kD;
 #pragma unroll
     for (int m = 0; m < 2; m++) {
@@ -525,7 +619,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     // the ring yet). Rows beyond it are not read: their lanes write zeros, which meet a weight of zero (a dead slot may hold infinities
     // and NaN). A resource over the tile: a ring may be larger than 32-bit offsets reach.
     const int n_rows = has_new ? new_tau : live < kTile ? live : kTile;
-    const rsrc_t rows = make_rsrc(a.v_win + ((size_t)u * a.W_cap + slot0) * kD, (uint32_t)n_rows * (kD * 2));
+    const rsrc_t rows = make_rsrc(a.v_win + ((size_t)uw * a.W_cap + slot0) * kD, (uint32_t)n_rows * (kD * 2));
 #pragma unroll
     for (int j = 0; j < 8; j++)
       buf_load_to_lds16(rows, (MIXED && 4 * j + kq < lo ? 0x40000000u : 0u) + 256u * (4 * j + kq) + 16u * (col ^ (2 * kq) ^ ((j & 2) ? 8 : 0)), 0, &T[4 * j][0]);
@@ -804,8 +898,8 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   // ring slot of tile j between the fronts
   auto mixed_slot = [&](int j) { int wi = a.m_ring + j; wi = wi >= a.ring_tiles ? wi - a.ring_tiles : wi; return wi * kTile; };
   if (!early) {
-    int r = sp + wave * a.n_splits;                      // < the number of live tiles, since wave < n_win
-    const int r_step = kWaves * a.n_splits;
+    int r = PAGED ? wave : sp + wave * a.n_splits;       // < the number of live tiles, since wave < n_win
+    const int r_step = PAGED ? kWaves : kWaves * a.n_splits;
     int left = (n_win - wave + kWaves - 1) / kWaves;     // tiles of this wave
     for (int begin = 1; left > 0; left--, r += r_step) {
       asm volatile("" : "+s"(begin));     // (keeps the first pass from being compiled a second time: the code is read cold at the start of a launch)
@@ -891,7 +985,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     }
     if (has_packed) {   // claim the first packed tile now
       it = grab();
-      if (!late_tile) st.load(up, it < p_end ? it : p_end - 1, lane16);
+      if (!late_tile) load_tile(st, it, lane16);
     }
   }
   // (a condition of its own: as the else of the one above it would be laid out in front of it, and the loads above would then wait
@@ -900,7 +994,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   asm volatile("" : "+s"(early_s));
   if (early_s) {
     it = p_begin + (wave - n_win);
-    if (has_packed && !late_tile) st.load(up, it < p_end ? it : p_end - 1, lane16);
+    if (has_packed && !late_tile) load_tile(st, it, lane16);
     __builtin_amdgcn_sched_barrier(0);
     start_barrier();
     __builtin_amdgcn_sched_barrier(0);
@@ -1084,7 +1178,11 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
       // zero-point term: A rows 0..3 carry the zero-points of channel blocks 0..3, rows 4..15 are ones
       // and accumulate the sum of the numerators
       half8_t z8 = ones8;
-      if (col < 4) z8 = *reinterpret_cast<const half8_t*>(&L.v.zv[col][8 * kq]);
+      if constexpr (kIdsInLds) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));       // (nor has it one for this address)
+        if (col < 4) z8 = *reinterpret_cast<const half8_t*>(&L.v.zv[ln & 15][8 * (ln >> 4)]);
+      } else if (col < 4) z8 = *reinterpret_cast<const half8_t*>(&L.v.zv[col][8 * kq]);
       accZ = mfma16(z8, PB, accZ);
 #pragma unroll
       for (int m = 0; m < 8; m++) add_values(exact, vc, m, Bv[m >> 1]);
@@ -1324,7 +1422,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     }
     if constexpr (kLateTile) {
       Stage<KB, VB> first;       // (not st itself: what it holds without a packed tile would be kept)
-      if (has_packed) first.load(up, it < p_end ? it : p_end - 1, lane16);
+      if (has_packed) load_tile(first, it, lane16);
       st = first;
     }
   }
@@ -1344,7 +1442,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     // and 17.7; at 126 tiles the same within 1 %. The level from the number of the claimed tile alone, several steps at once: 17.6 and
     // 18.3.)
     int prio = 0, next_at = p_end;
-    if constexpr (kWaves == 8) {
+    if constexpr (kWaves == 8 && !PAGED) {
       if (a.even && p_end - p_begin > 12) {      // (a handful of tiles, 32 units of 8: 6.2 us without, 6.4 with)
         prio = 3;
         next_at = p_begin + ((p_end - p_begin) >> 1);
@@ -1353,7 +1451,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     }
     while (it < p_end) {
       const int ticket = grab_issue();
-      if constexpr (kWaves == 8) {
+      if constexpr (kWaves == 8 && !PAGED) {
         if (it >= next_at) {
           prio--;
           next_at = prio > 0 ? it + ((p_end - it) >> 1) : p_end;
@@ -1364,9 +1462,9 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
       }
       process(st);
       it = grab_take(ticket);
-      st.load(up, it < p_end ? it : p_end - 1, lane16);
+      load_tile(st, it, lane16);
     }
-    if constexpr (kWaves == 8) __builtin_amdgcn_s_setprio(0);
+    if constexpr (kWaves == 8 && !PAGED) __builtin_amdgcn_s_setprio(0);
   }
 
   {
@@ -1422,6 +1520,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     }
     if (col < G) *reinterpret_cast<float4_t*>(&s_wave[wave].o[col][16 * m + 4 * kq]) = o4;   // channels 16m + 4kq .. +3
   }
+  if constexpr (PAGED) lsum = spoiled ? __builtin_nanf("") : lsum;      // (of every head, whatever the other waves have)
   if (col < G && kq == 0) { R.m[wave][col] = mref; R.l[wave][col] = lsum; }
 
   // Wave w combines the waves' results of heads w, w + kWaves, ... of the block, a lane two channels: the weights 2^(m_w - M) once
@@ -1441,11 +1540,14 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   };
   uint16_t* outp = a.out + row0 * kD;
   // partial of split s, head hh of the block: [unit][block][split][head of the block] (blocks of 16: [unit][split][head of the group])
-  const size_t part0 = kWide<G> ? (size_t)u * a.n_splits * a.G + head0 : (size_t)uo * a.n_splits * G;
+  int part_rows = a.n_splits;
+  if constexpr (PAGED) part_rows = a.max_splits;
+  const size_t part0 = kWide<G> ? (size_t)u * part_rows * a.G + head0 : (size_t)uo * part_rows * G;
   const int part_step = kWide<G> ? a.G : G;
   auto part_at = [&](int s, int hh) { return a.part + (part0 + (size_t)s * part_step + hh) * (kD + 2); };
   auto put_out = [&](int hh, const float2_t& O, float Lsum) {
-    const half2_t v = {(half_t)(O[0] / Lsum), (half_t)(O[1] / Lsum)};
+    half2_t v = {(half_t)(O[0] / Lsum), (half_t)(O[1] / Lsum)};
+    if (PAGED && Lsum == 0.0f) v = half2_t{0, 0};       // no tokens
     reinterpret_cast<uint32_t*>(outp + hh * kD)[lane] = as_u32(v);
   };
 
@@ -1663,6 +1765,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   }
 }
 
+#if !KVMIX_PAGED
 template <int KB, int VB>
 hipError_t launch_g(const AttnArgs& a, int G, dim3 grid, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
@@ -1674,24 +1777,41 @@ hipError_t launch_g(const AttnArgs& a, int G, dim3 grid, hipStream_t s) {
     e = launch(kernel, grid, kNW * kWave, s, a.q, a.packed, shares, items, heads, a);
   };
   switch (G) {
-    case 1: run(decode_attn_kernel<KB, VB, 1, kNW, kMixed>); break;
-    case 2: run(decode_attn_kernel<KB, VB, 2, kNW, kMixed>); break;
-    case 4: run(decode_attn_kernel<KB, VB, 4, kNW, kMixed>); break;
+    case 1: run(decode_attn_kernel<KB, VB, 1, kNW, kMixed, false>); break;
+    case 2: run(decode_attn_kernel<KB, VB, 2, kNW, kMixed, false>); break;
+    case 4: run(decode_attn_kernel<KB, VB, 4, kNW, kMixed, false>); break;
 #if !KVMIX_MIXED
     case 8:
       // (a block of 8 heads with 3- or 4-bit Values has 12 waves: attn_waves)
-      if constexpr (kNW == 12 || VB < 3) { run(decode_attn_kernel<KB, VB, 8, kNW, kMixed>); break; }
+      if constexpr (kNW == 12 || VB < 3) { run(decode_attn_kernel<KB, VB, 8, kNW, kMixed, false>); break; }
       else break;
 #endif
 #if KVMIX_WAVES == 8 || KVMIX_MIXED
-    case 16: run(decode_attn_kernel<KB, VB, 16, kNW, kMixed>); break;
+    case 16: run(decode_attn_kernel<KB, VB, 16, kNW, kMixed, false>); break;
 #endif
   }
   return e;
 }
 
+#else
+template <int KB, int VB>
+hipError_t launch_g(const PagedAttnArgs& a, u32x4_t shares, u32x4_t items, int block, dim3 grid, hipStream_t s) {
+  const u32x2_t heads = {(uint32_t)a.G, (uint32_t)a.head_blocks};
+  auto run = [&](auto kernel) { return launch(kernel, grid, kNW * kWave, s, a.q, a.packed, shares, items, heads, a); };
+  switch (block) {
+    case 1: return run(decode_attn_kernel<KB, VB, 1, kNW, false, true>);
+    case 2: return run(decode_attn_kernel<KB, VB, 2, kNW, false, true>);
+    case 4: return run(decode_attn_kernel<KB, VB, 4, kNW, false, true>);
+    case 8: if constexpr (VB < 3) return run(decode_attn_kernel<KB, VB, 8, kNW, false, true>); break;
+    case 16: return run(decode_attn_kernel<KB, VB, 16, kNW, false, true>);
+  }
+  return hipErrorInvalidValue;
+}
+#endif
+
 }  // namespace
 
+#if !KVMIX_PAGED
 template <>
 hipError_t launch_decode_attn<kNW, kMixed>(const AttnArgs& a, int k_bits, int v_bits, int block, int units, hipStream_t s) {
   const dim3 grid(a.n_splits, units, a.head_blocks);
@@ -1715,5 +1835,36 @@ hipError_t launch_decode_attn<kNW, kMixed>(const AttnArgs& a, int k_bits, int v_
   }
   return hipErrorInvalidValue;
 }
+#else
+hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int chunk_log2, int k_bits, int v_bits, int block, int B, hipStream_t s) {
+  const dim3 grid(a.Hkv * a.head_blocks, B, a.max_splits);
+  auto words = [](const int32_t* x, const int32_t* y) {
+    const uint64_t p = reinterpret_cast<uint64_t>(x), q = reinterpret_cast<uint64_t>(y);
+    return u32x4_t{(uint32_t)p, (uint32_t)(p >> 32), (uint32_t)q, (uint32_t)(q >> 32)};
+  };
+  const u32x4_t shares = words(rows, pages.lens);
+  u32x4_t items = words(pages.table, nullptr);
+  items[2] = (uint32_t)pages.max_tiles; items[3] = (uint32_t)chunk_log2 | (uint32_t)a.Hkv << 8;
+  switch (k_bits * 10 + v_bits) {
+    case 11: return launch_g<1, 1>(a, shares, items, block, grid, s);
+    case 12: return launch_g<1, 2>(a, shares, items, block, grid, s);
+    case 13: return launch_g<1, 3>(a, shares, items, block, grid, s);
+    case 14: return launch_g<1, 4>(a, shares, items, block, grid, s);
+    case 21: return launch_g<2, 1>(a, shares, items, block, grid, s);
+    case 31: return launch_g<3, 1>(a, shares, items, block, grid, s);
+    case 41: return launch_g<4, 1>(a, shares, items, block, grid, s);
+    case 22: return launch_g<2, 2>(a, shares, items, block, grid, s);
+    case 23: return launch_g<2, 3>(a, shares, items, block, grid, s);
+    case 24: return launch_g<2, 4>(a, shares, items, block, grid, s);
+    case 32: return launch_g<3, 2>(a, shares, items, block, grid, s);
+    case 33: return launch_g<3, 3>(a, shares, items, block, grid, s);
+    case 34: return launch_g<3, 4>(a, shares, items, block, grid, s);
+    case 42: return launch_g<4, 2>(a, shares, items, block, grid, s);
+    case 43: return launch_g<4, 3>(a, shares, items, block, grid, s);
+    case 44: return launch_g<4, 4>(a, shares, items, block, grid, s);
+  }
+  return hipErrorInvalidValue;
+}
+#endif
 
 }  // namespace kvmix

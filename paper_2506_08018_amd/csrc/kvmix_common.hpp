@@ -159,6 +159,51 @@ struct AttnArgs {
   bool even;              // the workgroups that share a compute unit keep pace with each other (8 waves)
 };
 
+// Paged attention: the fields above that depend on the sequence are filled in by the kernel.
+struct PagedAttnArgs : AttnArgs {
+  int n_slots, n_pages, Hkv, window, max_len;
+  int max_splits;         // grid z, and the stride of the partials
+  uint32_t ring_magic;    // floor(2^32 / ring_tiles) + 1 (0 for one ring tile): tile % ring_tiles without a division
+};
+// floor(t / n) for the magic number of n >= 2, t * n < 2^32; tile % ring_tiles of a launch
+__device__ __forceinline__ int ring_tile(int t, int ring_tiles, uint32_t magic) {
+  return magic ? t - ring_tiles * (int)__umulhi((uint32_t)t, magic) : 0;
+}
+// A word that no workgroup of the launch writes, at an address that is the same for the whole wave: read by a scalar load.
+__device__ __forceinline__ int load_uniform(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p));
+}
+// packed tiles of a sequence of n tokens
+__host__ __device__ __forceinline__ int packed_tiles(int n, int window) { return n - window < kTile ? 0 : (n - window) / kTile; }
+
+struct PagedAppendArgs {
+  QuantArgs q;            // inputs, strides of the Keys, rings, W_cap, pool, Hkv; the rest is filled in by the kernel
+  int64_t v_tok, v_head;
+  const int32_t* rows; const int32_t* cu; const int32_t* lens; const int32_t* grown; const int32_t* table;
+  int32_t* status;
+  int n_slots, n_pages, max_tiles, window, max_new;
+  int ring_tiles;
+  uint32_t ring_magic;
+};
+
+struct RopeSide { const void* in; uint16_t* out; const void* weight; int64_t tok, head; int heads; };
+struct RopeArgs {
+  RopeSide side[3];       // q, k, v
+  const int32_t* positions; const float* frequencies;
+  int n_tokens, rotary_dim, interleaved;
+  float amplitude, eps;
+};
+
+struct CopyArgs {         // rows of `bytes` bytes (a multiple of 16) inside one buffer or two, from index src[i] to dst[i]
+  char* base[2];
+  int n_base;
+  int64_t bytes;
+  const int32_t* src; const int32_t* dst;
+  const int32_t* count;   // NULL: n
+  int n, limit;           // indices outside [0, limit) are left out
+  int32_t* status;        // may be NULL
+};
+
 // A launch by hipLaunchKernel itself, without the configuration that <<<>>> pushes and pops (host time of a decode step of one
 // launch 5.6 -> 5.3 us, with the preloaded parameters as few as they can be: passed one by one, 13 of them, it was 5.8).
 template <typename... Params, typename... Args>
@@ -186,5 +231,20 @@ hipError_t launch_decode_attn(const AttnArgs& a, int k_bits, int v_bits, int blo
 template <> hipError_t launch_decode_attn<8, false>(const AttnArgs& a, int k_bits, int v_bits, int block, int units, hipStream_t s);
 template <> hipError_t launch_decode_attn<12, false>(const AttnArgs& a, int k_bits, int v_bits, int block, int units, hipStream_t s);
 template <> hipError_t launch_decode_attn<12, true>(const AttnArgs& a, int k_bits, int v_bits, int block, int units, hipStream_t s);
+
+
+hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int chunk_log2, int k_bits, int v_bits, int block, int B, hipStream_t s);
+hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, int B, hipStream_t s);
+hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t s);
+hipError_t launch_pages_grow(const kvmix_pages& p, const int32_t* rows, const int32_t* cu, int n, hipStream_t s);
+hipError_t launch_pages_free(const kvmix_pages& p, const int32_t* rows, int n, hipStream_t s);
+hipError_t launch_pages_fork(const kvmix_pages& p, const int32_t* src, const int32_t* dst, int n, hipStream_t s);
+hipError_t launch_pages_compact(const kvmix_pages& p, hipStream_t s);
+hipError_t launch_copy(const CopyArgs& a, hipStream_t s);
+
+// Host checks that the entry points share (kvmix_api.hip).
+int hip_fail(hipError_t e);
+int check_shape_cfg(const kvmix_shape* sh, const kvmix_layer_cfg* cfg);
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace kvmix

@@ -1,0 +1,306 @@
+// C-ABI entry points of the paged cache and of what stands in front of it: host-side validation and launch plumbing only.
+// Contract: include/kvmix.h.
+#include <cmath>
+#include "kvmix_common.hpp"
+
+using namespace kvmix;
+
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int check_pages(const kvmix_pages* p) {
+  if (!p || !p->table || !p->lens || !p->grown || !p->refs || !p->used || !p->status) return KVMIX_ERR_NULL;
+  if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->grown) || !aligned4(p->refs) || !aligned4(p->used) || !aligned4(p->status)) return KVMIX_ERR_ALIGN;
+  // (page counts to 4 M: the grow kernel keeps one of 1024 counters for every 4096)
+  if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages > (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 26)) return KVMIX_ERR_BAD_SHAPE;
+  if (p->window < 0 || p->window % kTile) return KVMIX_ERR_BAD_SHAPE;
+  return KVMIX_OK;
+}
+
+int check_paged_cfg(const kvmix_shape* sh, const kvmix_layer_cfg* cfg) {
+  const int st = check_shape_cfg(sh, cfg);
+  if (st) return st;
+  if (cfg->k_bits == 16) return KVMIX_ERR_BAD_BITS;
+  return cfg->window < 0 ? KVMIX_ERR_BAD_SHAPE : KVMIX_OK;
+}
+
+// `pool`, `rings`: what the call touches
+int check_paged_cache(const kvmix_layer_cfg* cfg, const kvmix_paged_cache* c, bool pool, bool rings) {
+  if (!c || (pool && !c->pool) || (rings && (!c->k_win || !c->v_win))) return KVMIX_ERR_NULL;
+  if ((pool && !aligned16(c->pool)) || (rings && (!aligned16(c->k_win) || !aligned16(c->v_win)))) return KVMIX_ERR_ALIGN;
+  if (c->n_pages < 1 || c->n_slots < 1 || c->W_cap % kTile || c->W_cap < cfg->window + kTile) return KVMIX_ERR_BAD_SHAPE;
+  return KVMIX_OK;
+}
+
+int check_together(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const kvmix_paged_cache* c, const kvmix_pages* p) {
+  if (c->n_pages != p->n_pages || c->n_slots != p->n_slots || cfg->window != p->window) return KVMIX_ERR_BAD_SHAPE;
+  // tile % ring tiles goes by a product with a reciprocal; (slot, head) pairs are counted in 32 bits
+  if ((long long)p->max_tiles * (c->W_cap / kTile) >= (1LL << 32) || (long long)p->n_slots * sh->Hkv > 0x7fffffffLL) return KVMIX_ERR_BAD_SHAPE;
+  return KVMIX_OK;
+}
+
+uint32_t ring_magic(int ring_tiles) { return ring_tiles == 1 ? 0u : (uint32_t)((1ULL << 32) / (uint32_t)ring_tiles + 1); }
+
+// How a ragged launch shares out contexts of up to max_len tokens.
+struct PagedPlan { int block, head_blocks, log2, splits; size_t counters, bytes; };
+PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits) {
+  PagedPlan p;
+  const int G = sh->Hq / sh->Hkv, units = sh->B * sh->Hkv;
+  p.block = G <= 4 || (G == 8 && v_bits < 3) ? G : 16;
+  p.head_blocks = (G + p.block - 1) / p.block;
+  const int tiles = packed_tiles(max_len, window), held = max_len < window + kTile ? max_len : window + kTile - 1;
+  const int win = 3 * ((held + kTile - 1) / kTile);
+  const long long work = (long long)units * p.head_blocks * (tiles + win);
+  for (p.log2 = 3; p.log2 < 6 && (long long)512 << p.log2 < work; p.log2++) {}
+  auto count = [&]() {
+    const int share = 1 << p.log2;
+    return (int)(((long long)tiles + (win < share ? win : share) + share - 1) >> p.log2);
+  };
+  while (count() > 1024) p.log2++;
+  p.splits = count() < 1 ? 1 : count();
+  p.counters = ((size_t)units * (G > 8 ? G / 8 : 1) * 4 + 255) / 256 * 256;
+  p.bytes = p.counters + (size_t)units * p.splits * G * (kD + 2) * sizeof(float);
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvmix_pages_grow(const kvmix_pages* p, const int32_t* rows, const int32_t* cu, int n_rows, void* stream) {
+  const int st = check_pages(p);
+  if (st) return st;
+  if (n_rows < 0 || n_rows > 4096) return KVMIX_ERR_BAD_SHAPE;
+  if (!aligned4(rows) || !aligned4(cu)) return KVMIX_ERR_ALIGN;
+  if (n_rows == 0) return KVMIX_OK;
+  const hipError_t e = launch_pages_grow(*p, rows, cu, n_rows, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_pages_free(const kvmix_pages* p, const int32_t* rows, int n_rows, void* stream) {
+  const int st = check_pages(p);
+  if (st) return st;
+  if (n_rows < 0 || n_rows > (1 << 20)) return KVMIX_ERR_BAD_SHAPE;
+  if (!aligned4(rows)) return KVMIX_ERR_ALIGN;
+  if (n_rows == 0) return KVMIX_OK;
+  const hipError_t e = launch_pages_free(*p, rows, n_rows, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_pages_fork(const kvmix_pages* p, const int32_t* src, const int32_t* dst, int n_pairs, void* stream) {
+  const int st = check_pages(p);
+  if (st) return st;
+  if (n_pairs < 0 || n_pairs > 4096) return KVMIX_ERR_BAD_SHAPE;
+  if (n_pairs == 0) return KVMIX_OK;
+  if (!src || !dst) return KVMIX_ERR_NULL;
+  if (!aligned4(src) || !aligned4(dst)) return KVMIX_ERR_ALIGN;
+  const hipError_t e = launch_pages_fork(*p, src, dst, n_pairs, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_pages_compact(const kvmix_pages* p, void* stream) {
+  const int st = check_pages(p);
+  if (st) return st;
+  if (!p->moves) return KVMIX_ERR_NULL;
+  if (!aligned16(p->moves)) return KVMIX_ERR_ALIGN;
+  const hipError_t e = launch_pages_compact(*p, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_move_records(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const kvmix_paged_cache* c, const kvmix_pages* p, void* stream) {
+  int st = check_paged_cfg(sh, cfg);
+  if (st) return st;
+  st = check_paged_cache(cfg, c, true, false);
+  if (st) return st;
+  st = check_pages(p);
+  if (st) return st;
+  st = check_together(sh, cfg, c, p);
+  if (st) return st;
+  if (!p->moves) return KVMIX_ERR_NULL;
+  if (!aligned16(p->moves)) return KVMIX_ERR_ALIGN;
+  CopyArgs a{};
+  a.base[0] = reinterpret_cast<char*>(c->pool);
+  a.n_base = 1;
+  a.bytes = (int64_t)sh->Hkv * record_words(cfg->k_bits, cfg->v_bits) * 4;
+  a.src = p->moves + 4; a.dst = a.src + p->n_pages; a.count = p->moves;
+  a.n = p->n_pages / 2 + 1;      // no more moves than gaps and no more than pages above them
+  a.limit = p->n_pages;
+  a.status = p->status;
+  const hipError_t e = launch_copy(a, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_copy_windows(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const kvmix_paged_cache* c, const int32_t* src, const int32_t* dst,
+                       int n_pairs, void* stream) {
+  int st = check_paged_cfg(sh, cfg);
+  if (st) return st;
+  st = check_paged_cache(cfg, c, false, true);
+  if (st) return st;
+  if (n_pairs < 0 || n_pairs > 65535) return KVMIX_ERR_BAD_SHAPE;
+  if (n_pairs == 0) return KVMIX_OK;
+  if (!src || !dst) return KVMIX_ERR_NULL;
+  if (!aligned4(src) || !aligned4(dst)) return KVMIX_ERR_ALIGN;
+  CopyArgs a{};
+  a.base[0] = reinterpret_cast<char*>(c->k_win);
+  a.base[1] = reinterpret_cast<char*>(c->v_win);
+  a.n_base = 2;
+  a.bytes = (int64_t)sh->Hkv * c->W_cap * kD * 2;
+  a.src = src; a.dst = dst;
+  a.n = n_pairs; a.limit = c->n_slots;
+  const hipError_t e = launch_copy(a, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_paged_append(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const uint16_t* k_new, int64_t k_token_stride, int64_t k_head_stride,
+                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride, const kvmix_paged_cache* c, const kvmix_pages* p, const int32_t* rows, const int32_t* cu, int max_new,
+                       void* stream) {
+  int st = check_paged_cfg(sh, cfg);
+  if (st) return st;
+  st = check_paged_cache(cfg, c, true, true);
+  if (st) return st;
+  st = check_pages(p);
+  if (st) return st;
+  st = check_together(sh, cfg, c, p);
+  if (st) return st;
+  if (max_new < 0 || (!cu && max_new > 1)) return KVMIX_ERR_BAD_SHAPE;
+  if (!aligned4(rows) || !aligned4(cu)) return KVMIX_ERR_ALIGN;
+  if (max_new == 0) return KVMIX_OK;
+  if (!k_new || !v_new) return KVMIX_ERR_NULL;
+  if (!aligned16(k_new) || !aligned16(v_new)) return KVMIX_ERR_ALIGN;
+  for (const int64_t x : {k_token_stride, k_head_stride, v_token_stride, v_head_stride})
+    if (x % 8 || x < 0) return KVMIX_ERR_ALIGN;
+  if (!rows && p->n_slots < sh->B) return KVMIX_ERR_BAD_SHAPE;
+  PagedAppendArgs a{};
+  a.q.k = k_new; a.q.v = v_new;
+  a.q.tok = k_token_stride; a.q.unit_h = k_head_stride;
+  a.v_tok = v_token_stride; a.v_head = v_head_stride;
+  a.q.k_ring = c->k_win; a.q.v_ring = c->v_win; a.q.k_ring_w = c->k_win; a.q.v_ring_w = c->v_win;
+  a.q.W_cap = c->W_cap; a.q.packed = c->pool; a.q.Hkv = sh->Hkv;
+  a.rows = rows; a.cu = cu; a.lens = p->lens; a.grown = p->grown; a.table = p->table; a.status = p->status;
+  a.n_slots = p->n_slots; a.n_pages = p->n_pages; a.max_tiles = p->max_tiles; a.window = p->window; a.max_new = max_new;
+  a.ring_tiles = c->W_cap / kTile;
+  a.ring_magic = ring_magic(a.ring_tiles);
+  const hipError_t e = launch_paged_append(a, cfg->k_bits, cfg->v_bits, sh->B, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_paged_workspace_bytes(const kvmix_shape* sh, int max_len, size_t* bytes) {
+  const kvmix_layer_cfg cfg = {2, 2, 0};
+  const int st = check_shape_cfg(sh, &cfg);
+  if (st) return st;
+  if (!bytes) return KVMIX_ERR_NULL;
+  if (max_len < 1) return KVMIX_ERR_BAD_SHAPE;
+  // any window and any widths: the most splits over both (a window packs fewer tiles; its own are at most one share more)
+  *bytes = 0;
+  for (int v_bits = 2; v_bits <= 3; v_bits++) {
+    PagedPlan p = plan_paged(sh, 0, max_len, v_bits);
+    const size_t more = p.bytes + (size_t)sh->B * sh->Hkv * 2 * (sh->Hq / sh->Hkv) * (kD + 2) * sizeof(float);
+    if (more > *bytes) *bytes = more;
+  }
+  return KVMIX_OK;
+}
+
+int kvmix_paged_decode_attn(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const uint16_t* q, const kvmix_paged_cache* c, const kvmix_pages* p,
+                            const int32_t* rows, int max_len, float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  int st = check_paged_cfg(sh, cfg);
+  if (st) return st;
+  if (!q || !out) return KVMIX_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out)) return KVMIX_ERR_ALIGN;
+  st = check_paged_cache(cfg, c, true, true);
+  if (st) return st;
+  st = check_pages(p);
+  if (st) return st;
+  st = check_together(sh, cfg, c, p);
+  if (st) return st;
+  if (!aligned4(rows)) return KVMIX_ERR_ALIGN;
+  if (!rows && p->n_slots < sh->B) return KVMIX_ERR_BAD_SHAPE;
+  const long long most = (long long)p->max_tiles * kTile + p->window + kTile - 1;
+  if (max_len <= 0 || max_len > most) max_len = most < 0x7fffffffLL ? (int)most : 0x7fffffff;
+  const PagedPlan plan = plan_paged(sh, p->window, max_len, cfg->v_bits);
+  PagedAttnArgs a{};
+  if (plan.splits > 1) {
+    if (!workspace) return KVMIX_ERR_NULL;
+    if (!aligned16(workspace)) return KVMIX_ERR_ALIGN;
+    if (workspace_bytes < plan.bytes) return KVMIX_ERR_WORKSPACE;
+    a.counters = reinterpret_cast<uint32_t*>(workspace);
+    a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + plan.counters);
+  }
+  const int G = sh->Hq / sh->Hkv, counted = sh->B * sh->Hkv * (G > 8 ? G / 8 : 1);
+  a.counter_stride = 1;
+  while (a.counter_stride * 2 * counted <= 64) a.counter_stride *= 2;
+  a.q = q; a.out = out; a.G = G;
+  a.packed = c->pool;
+  a.k_win = c->k_win; a.v_win = c->v_win;
+  a.W_cap = c->W_cap; a.ring_tiles = c->W_cap / kTile;
+  a.head_blocks = plan.head_blocks;
+  a.max_splits = plan.splits;
+  a.n_slots = p->n_slots; a.n_pages = p->n_pages; a.Hkv = sh->Hkv; a.window = p->window; a.max_len = max_len;
+  a.ring_magic = ring_magic(a.ring_tiles);
+  const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)kD);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const hipError_t e = launch_paged_attn(a, *p, rows, plan.log2, cfg->k_bits, cfg->v_bits, plan.block, sh->B, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+int kvmix_rope_frequencies(int rotary_dim, double base, int scaling, double factor, int original_len, double low, double high, float* frequencies,
+                           float* amplitude) {
+  if (!frequencies) return KVMIX_ERR_NULL;
+  if (rotary_dim < 2 || rotary_dim > kD || rotary_dim % 2 || !(base > 1.0) || !std::isfinite(base)) return KVMIX_ERR_BAD_SHAPE;
+  if (scaling < KVMIX_ROPE_PLAIN || scaling > KVMIX_ROPE_INDEX) return KVMIX_ERR_BAD_SHAPE;
+  if (scaling != KVMIX_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return KVMIX_ERR_BAD_SHAPE;
+  const bool ramps = scaling == KVMIX_ROPE_TURNS || scaling == KVMIX_ROPE_INDEX;
+  if (ramps && (original_len < 1 || !(low > 0.0) || !(high > low) || !std::isfinite(high))) return KVMIX_ERR_BAD_SHAPE;
+  if (scaling == KVMIX_ROPE_BASE && rotary_dim == 2) return KVMIX_ERR_BAD_SHAPE;
+  const double two_pi = 6.283185307179586477, r = rotary_dim;
+  if (scaling == KVMIX_ROPE_BASE) base *= std::pow(factor, r / (r - 2));
+  // index at which a pair makes `turns` turns in original_len positions: original_len * base^(-2i / r) = 2 pi turns
+  auto index_of = [&](double turns) { return r * std::log(original_len / (two_pi * turns)) / (2.0 * std::log(base)); };
+  for (int i = 0; i < rotary_dim / 2; i++) {
+    const double f = std::pow(base, -2.0 * i / r);
+    double keep = 1.0;               // share of the unscaled frequency
+    if (scaling == KVMIX_ROPE_LINEAR) keep = 0.0;
+    if (scaling == KVMIX_ROPE_TURNS) keep = (original_len * f / two_pi - low) / (high - low);
+    if (scaling == KVMIX_ROPE_INDEX) keep = (index_of(low) - i) / (index_of(low) - index_of(high));
+    keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+    frequencies[i] = (float)(scaling == KVMIX_ROPE_PLAIN || scaling == KVMIX_ROPE_BASE ? f : f * keep + f / factor * (1.0 - keep));
+  }
+  if (amplitude) *amplitude = scaling == KVMIX_ROPE_INDEX ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return KVMIX_OK;
+}
+
+int kvmix_qk_norm_rope(const kvmix_shape* sh, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions, const void* q,
+                       int64_t q_token_stride, int64_t q_head_stride, uint16_t* q_out, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                       uint16_t* k_out, const void* v, int64_t v_token_stride, int64_t v_head_stride, uint16_t* v_out, void* stream) {
+  const kvmix_layer_cfg cfg = {2, 2, 0};
+  const int st = check_shape_cfg(sh, &cfg);
+  if (st) return st;
+  if (!rope) return KVMIX_ERR_NULL;
+  if (dtype != KVMIX_F16 && dtype != KVMIX_BF16 && dtype != KVMIX_F32) return KVMIX_ERR_BAD_SHAPE;
+  if (rope->rotary_dim < 0 || rope->rotary_dim > kD || rope->rotary_dim % 16 || n_tokens < 0) return KVMIX_ERR_BAD_SHAPE;
+  if (!(rope->eps >= 0.0f)) return KVMIX_ERR_BAD_SHAPE;
+  if (rope->rotary_dim > 0 && !rope->frequencies) return KVMIX_ERR_NULL;
+  if (!aligned16(rope->frequencies) || !aligned16(rope->q_weight) || !aligned16(rope->k_weight) || !aligned4(positions)) return KVMIX_ERR_ALIGN;
+  const int step = dtype == KVMIX_F32 ? 4 : 8;       // elements of 16 bytes
+  RopeArgs a{};
+  const void* in[3] = {q, k, v};
+  uint16_t* out[3] = {q_out, k_out, v_out};
+  const void* weight[3] = {rope->q_weight, rope->k_weight, nullptr};
+  const int64_t tok[3] = {q_token_stride, k_token_stride, v_token_stride}, head[3] = {q_head_stride, k_head_stride, v_head_stride};
+  for (int i = 0; i < 3; i++) {
+    if (!in[i] != !out[i]) return KVMIX_ERR_NULL;
+    if (!aligned16(in[i]) || !aligned16(out[i]) || (in[i] && (tok[i] % step || head[i] % step))) return KVMIX_ERR_ALIGN;
+    a.side[i] = RopeSide{in[i], out[i], weight[i], tok[i], head[i], !in[i] ? 0 : i == 0 ? sh->Hq : sh->Hkv};
+  }
+  if (n_tokens == 0 || (!q && !k && !v)) return KVMIX_OK;
+  if (!positions && rope->rotary_dim > 0 && (q || k)) return KVMIX_ERR_NULL;
+  a.positions = positions; a.frequencies = rope->frequencies;
+  a.n_tokens = n_tokens; a.interleaved = rope->interleaved != 0;
+  a.rotary_dim = q || k ? rope->rotary_dim : 0;
+  a.amplitude = rope->amplitude; a.eps = rope->eps;
+  const hipError_t e = launch_rope(a, dtype, (hipStream_t)stream);
+  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+}
+
+}  // extern "C"

@@ -336,9 +336,14 @@ __device__ __forceinline__ T load_row(const uint16_t* p) {
 // 32 elements instead of 64, one after the other: of the 3.5 us (4.6 at most, where exact ties are settled) that a tile alone took
 // in two waves from its start to its last store, the parameters of the groups were 0.45, the codes 1.05 (with ties 2.3) and the
 // words 0.4.
-template <int KB, int VB, bool PARTIAL, int SPLIT, Stream S>
+//
+// InPlace: the tile's place in a contiguous cache, from the grid; or a Paged one that the caller found.
+struct InPlace {};
+struct Paged { int unit; uint32_t* record; };       // unit: (slot, kv head) of the rings
+template <int KB, int VB, bool PARTIAL, int SPLIT, Stream S, typename Place = InPlace>
 __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16_t* v_in, int64_t tok, int64_t unit_b, int64_t unit_h, uint32_t* packed,
-                                              int n_tiles, int n_ring, const QuantArgs& a) {
+                                              int n_tiles, int n_ring, const QuantArgs& a, Place place = {}) {
+  constexpr bool PAGED = std::is_same_v<Place, Paged>;
   constexpr int kWords = 16 / SPLIT;           // words of a column group, per wave
   __shared__ __attribute__((aligned(16))) uint32_t s_key[512];             // the Key section's image
   __shared__ __attribute__((aligned(16))) uint32_t s_value[kTile * kD / 2];   // the Value rows, then the Value section's image
@@ -351,11 +356,15 @@ __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16
   const int side = wave / SPLIT, part = wave % SPLIT;      // side: 0 Keys, 1 Values
   const int kq = lane >> 4, j = (lane >> 2) & 3, q = lane & 3;
   const int tile_in = blockIdx.x, jh = blockIdx.y, b = blockIdx.z;   // no integer division at the start of a short kernel
-  const uint16_t* in = (side ? v_in : k_in) + b * unit_b + jh * unit_h;
+  const uint16_t* in = (side ? v_in : k_in) + (PAGED ? 0 : b * unit_b) + jh * unit_h;
+  auto unit = [&]() {
+    if constexpr (PAGED) return place.unit;
+    else return b * a.Hkv + jh;
+  };
   // Input row i (of those that stay in the window) to its ring slot: rows 16 bytes per lane, four at a time. from: ring slot, counted from
   // ring_w0, of the first of 32 slots; the slots [lo, hi) of them are this workgroup's to fill.
   auto copy_rows = [&](int from, int lo, int hi) {
-    uint16_t* ring_w = (side ? a.v_ring_w : a.k_ring_w) + (size_t)(b * a.Hkv + jh) * a.W_cap * kD;
+    uint16_t* ring_w = (side ? a.v_ring_w : a.k_ring_w) + (size_t)unit() * a.W_cap * kD;
     u32x4_t x[8 / SPLIT];
     int at[8 / SPLIT];
 #pragma unroll
@@ -407,7 +416,7 @@ __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16
   } else if (n_old > 0) {
     int slot0 = a.ring_w0 + tile_in * kTile;
     if (slot0 >= a.W_cap) slot0 -= a.W_cap;
-    old_rows = (side ? a.v_ring : a.k_ring) + ((int64_t)(b * a.Hkv + jh) * a.W_cap + slot0) * kD;
+    old_rows = (side ? a.v_ring : a.k_ring) + ((int64_t)unit() * a.W_cap + slot0) * kD;
   }
   // a tile all of one kind, the usual case
   const bool whole = PARTIAL || n_old >= kTile || n_old <= 0;
@@ -420,7 +429,10 @@ __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16
     __builtin_amdgcn_sched_barrier(0);
   };
   // (packed: of the launch's first tile)
-  auto record = [&]() { return packed + ((size_t)(b * a.Hkv + jh) * a.tiles_cap + (size_t)tile_in) * record_words(KB, VB); };
+  auto record = [&]() {
+    if constexpr (PAGED) return place.record;
+    else return packed + ((size_t)(b * a.Hkv + jh) * a.tiles_cap + (size_t)tile_in) * record_words(KB, VB);
+  };
   uint32_t hi[kWords];
 #pragma unroll
   for (int i = 0; i < kWords; i++) hi[i] = 0;
@@ -695,6 +707,45 @@ __global__ __launch_bounds__(128, 4) void quantize_pack_many_kernel(QuantArgs a)
   quantize_tile<KB, VB, PARTIAL, 1, S>(a.k, a.v, a.tok, a.unit_b, a.unit_h, a.packed + (size_t)a.tile0 * record_words(KB, VB), a.n_tiles, a.n_ring, a);
 }
 
+// A paged, ragged append: grid (due tiles and ring tiles, kv heads, batch rows). What kvmix_append_tokens works out on the host for
+// a batch of one length is worked out here for each sequence, from its length: the tiles that fall due, which page each goes to, and
+// the new rows that stay. Workgroups that their sequence has no work for end at once.
+template <int KB, int VB, int SPLIT, Stream S>
+__global__ __launch_bounds__(128 * SPLIT, 4) void paged_append_kernel(PagedAppendArgs p) {
+  const int b = blockIdx.z, jh = blockIdx.y, x = blockIdx.x;
+  const int row = p.rows ? load_uniform(p.rows + b) : b;
+  if (row < 0) return;
+  if (row >= p.n_slots) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
+  const int first = p.cu ? load_uniform(p.cu + b) : b, n_new = p.cu ? load_uniform(p.cu + b + 1) - first : 1;
+  const int n = load_uniform(p.lens + row), grown = load_uniform(p.grown + row);
+  if (n_new <= 0 || grown == 0) return;       // (a row that was not granted its tokens has said so)
+  if (n_new != grown || n_new > p.max_new || n < n_new || first < 0) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
+  QuantArgs a = p.q;
+  const int old_tiles = packed_tiles(n - n_new, p.window), tiles = packed_tiles(n, p.window), due = tiles - old_tiles;
+  if (tiles > p.max_tiles) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
+  const int n_ring = n - n_new - old_tiles * kTile;       // old tokens in the ring
+  const int kept_from = due * kTile;                       // first row (ring, then input) that stays
+  a.ring_w0 = ring_tile(old_tiles, p.ring_tiles, p.ring_magic) * kTile;
+  a.copy_row = kept_from > n_ring ? kept_from - n_ring : 0;
+  a.n_copy = n_new - a.copy_row;
+  a.copy_at = kept_from > n_ring ? ring_tile(due, p.ring_tiles, p.ring_magic) * kTile : n_ring;
+  const int n_read = kept_from < n_ring ? kept_from : n_ring, end = a.copy_at + a.n_copy;
+  a.n_read = a.copy_at < n_read || end > a.W_cap ? n_read : 0;
+  const int from = end - a.W_cap > n_read || a.copy_at < n_read ? n_read : a.copy_at, to = end < a.W_cap ? end : a.W_cap;
+  a.copy_tile0 = from / kTile;
+  a.copy_tiles = a.n_copy > 0 && to > from ? (to + kTile - 1) / kTile - a.copy_tile0 : 0;
+  if (x >= due + a.copy_tiles) return;
+  Paged place{row * a.Hkv + jh, nullptr};
+  if (x < due) {
+    const int at = old_tiles + x, id = load_uniform(p.table + (size_t)row * p.max_tiles + at);
+    if ((uint32_t)id >= (uint32_t)p.n_pages) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ID); return; }
+    place.record = a.packed + ((size_t)id * a.Hkv + jh) * record_words(KB, VB);
+  }
+  const bool values = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= SPLIT;      // this wave's side
+  quantize_tile<KB, VB, false, SPLIT, S>(a.k + first * a.tok, a.v + first * p.v_tok, values ? p.v_tok : a.tok, 0, values ? p.v_head : a.unit_h, nullptr,
+                                         due, n_ring, a, place);
+}
+
 // x = code * s_i + min, evaluated in fp32 (multiply, then add), of the first n_tokens tokens of every unit.
 __global__ __launch_bounds__(256) void dequant_kernel(DequantArgs a) {
   const int u = blockIdx.y, tile_i = blockIdx.x;
@@ -812,7 +863,40 @@ hipError_t launch_bits(const QuantArgs& a, int k_bits, int v_bits, int n_tiles, 
   return hipErrorInvalidValue;
 }
 
+// Four waves or two to a tile, past the caches or not: as for quantize_pack, by the tiles that may fall due.
+template <int KB, int VB>
+hipError_t launch_pa(const PagedAppendArgs& a, int B, hipStream_t s) {
+  const int due = (a.max_new + kTile - 1) / kTile;
+  const dim3 grid(due + (a.max_new == 1 ? 1 : a.ring_tiles), a.q.Hkv, B);
+  const size_t tiles = (size_t)due * a.q.Hkv * B;
+  if (tiles < 2048) return launch(paged_append_kernel<KB, VB, 2, kCached>, grid, 4 * kWave, s, a);
+  if (tiles <= (KB == 3 || VB == 3 ? 4096 : 8192)) return launch(paged_append_kernel<KB, VB, 2, kStreamOut>, grid, 4 * kWave, s, a);
+  return launch(paged_append_kernel<KB, VB, 1, kStreamOut>, grid, 2 * kWave, s, a);
+}
+
 }  // namespace
+
+hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, int B, hipStream_t s) {
+  switch (k_bits * 10 + v_bits) {
+    case 11: return launch_pa<1, 1>(a, B, s);
+    case 12: return launch_pa<1, 2>(a, B, s);
+    case 13: return launch_pa<1, 3>(a, B, s);
+    case 14: return launch_pa<1, 4>(a, B, s);
+    case 21: return launch_pa<2, 1>(a, B, s);
+    case 22: return launch_pa<2, 2>(a, B, s);
+    case 23: return launch_pa<2, 3>(a, B, s);
+    case 24: return launch_pa<2, 4>(a, B, s);
+    case 31: return launch_pa<3, 1>(a, B, s);
+    case 32: return launch_pa<3, 2>(a, B, s);
+    case 33: return launch_pa<3, 3>(a, B, s);
+    case 34: return launch_pa<3, 4>(a, B, s);
+    case 41: return launch_pa<4, 1>(a, B, s);
+    case 42: return launch_pa<4, 2>(a, B, s);
+    case 43: return launch_pa<4, 3>(a, B, s);
+    case 44: return launch_pa<4, 4>(a, B, s);
+  }
+  return hipErrorInvalidValue;
+}
 
 hipError_t launch_quantize_pack(QuantArgs a, int k_bits, int v_bits, int n_tiles, int units, hipStream_t s) {
   a.n_tiles = n_tiles;
