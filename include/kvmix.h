@@ -366,12 +366,13 @@ int kvmix_paged_append(const kvmix_shape* shape, const kvmix_layer_cfg* cfg,
                        const kvmix_paged_cache* cache, const kvmix_pages* pages,
                        const int32_t* rows, const int32_t* cu, int max_new, void* stream);
 
-/* Workspace of kvmix_paged_decode_attn for lengths up to max_len: zero-filled once, for one shape and max_len; calls that overlap in time
- * need one each. */
+/* Workspace of kvmix_paged_decode_attn for lengths up to max_len, any window and any widths: zero-filled once, and again before it serves
+ * another shape; calls that overlap in time need one each (two captured graphs that may run at once, too). */
 int kvmix_paged_workspace_bytes(const kvmix_shape* shape, int max_len, size_t* bytes);
 /* kvmix_decode_attn for a ragged batch: q, out fp16 [shape->B][Hq][128], row b attends to the lens[s] tokens of slot s = rows[b]. A
  * sequence without tokens gives zeros; a padding row of out is left as it was; a length above max_len (<= 0: what a table row
- * holds) or a page id out of range gives NaN. Contexts are split over workgroups in shares of equal size and joined in the same launch. */
+ * holds) or a page id out of range gives NaN. Contexts are split over workgroups by the lengths that the device finds, and joined in the
+ * same launch (one launch for every 512 rows). With one row the split goes by max_len: a bound near the length is worth giving. */
 int kvmix_paged_decode_attn(const kvmix_shape* shape, const kvmix_layer_cfg* cfg, const uint16_t* q,
                             const kvmix_paged_cache* cache, const kvmix_pages* pages, const int32_t* rows, int max_len,
                             float softmax_scale, uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);

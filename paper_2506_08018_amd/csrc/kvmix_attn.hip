@@ -38,7 +38,6 @@ namespace {
 // 12 waves, one workgroup per CU: 168 registers per lane. 8 waves: 128 registers, two workgroups per CU.
 constexpr int kNW = KVMIX_WAVES;
 constexpr bool kMixed = KVMIX_MIXED;     // with tiles between a Key front and a Value front
-constexpr int kWindowTiles = 3;          // packed tiles that take a wave as long as one window tile (PAGED)
 constexpr int kMergeBatch = 32;          // splits whose partials the merging workgroup requests together (one round trip)
 // Reference of the running softmax (log2 units): numerators 2^(score - reference) are kept at or below 2^kRefCap;
 // when a score would exceed that, the reference is raised to (that score - kRefCap + 4), which leaves room for
@@ -380,6 +379,134 @@ template <int G> struct __attribute__((aligned(16))) WaveLds {
   union { Key k; Value v; };
 };
 
+// ---- PAGED: which piece of which context is a workgroup's, worked out by one of its waves from the lengths of the whole batch, which only
+// the device knows: a lane holds those of up to kBatchRows / 64 sequences. Pieces are tiles of a context, window tiles counted kWindowTiles each, a
+// context's all of one size and none larger than the share. The share is the best of four by a model of the launch (model_time). Shares of a size
+// that the host takes from the longest length leave either long contexts in few workgroups or short ones in many, and a workgroup for every
+// piece that a shorter context does not have: 17 x 8 units of 64 to 8192 tokens took 27.7, 20.8, 17.2, 21.5 and 34.3 us in shares of 8, 16,
+// 32, 64 and 128 tiles (15.5 this way), 512 units of 2048 to 4096 tokens 92, 68.8, 54.5, 49.6 and 43.6 (43), 256 units of 64 to 32 768
+// tokens 136, 86.7, 63, 52.6 and 49.9 (33). The price is 1.3 us at the start of every workgroup: the lengths' way from memory in front of the
+// page ids' and some 150 instructions of one wave (by every wave for itself, with seven shares tried one after the other, 1.9).
+constexpr int kBatchRows = 512;          // of one launch
+struct Piece { int row, slot, len, sp, splits, first, total, items_q, items_r, win_each, win_extra, win_tiles, n_w, tiles; };      // row -1: none; first: of the row's pieces
+template <int CTRL, int ROW_MASK = 0xf>
+__device__ __forceinline__ int dpp_i(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v) {      // inclusive
+  v += dpp_i<0x111>(v);    // row_shr
+  v += dpp_i<0x112>(v);
+  v += dpp_i<0x114>(v);
+  v += dpp_i<0x118>(v);
+  v += dpp_i<0x142, 0xA>(v);   // row_bcast:15, :31
+  v += dpp_i<0x143, 0xC>(v);
+  return v;
+}
+__device__ __forceinline__ float wave_max_dpp(float v) {      // of numbers that are not negative
+  v = row_max(v);
+  v = fmaxf(v, dpp_f<0x142, 0xA>(v));
+  v = fmaxf(v, dpp_f<0x143, 0xC>(v));
+  return uniform_lane(v, 63);
+}
+// a little less than 1 / d, so that a multiple of d times it rounds up to no more than the factor
+__device__ __forceinline__ float under_reciprocal(float d) { return __builtin_amdgcn_rcpf(d) * (1.0f - 0x1p-21f); }
+// x / d for 0 <= x < 2^24 and d > 0, rounded down (the product is off by one at most)
+__device__ __forceinline__ int quotient(int x, int d, float inv) {
+  int q = (int)((float)x * inv);
+  const int r = x - q * d;
+  q += r >= d ? 1 : 0;
+  return r < 0 ? q - 1 : q;
+}
+template <int N>
+__device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* lens, int n_rows, int n_ids, const PagedAttnArgs& a, int k, int lane) {
+  int slot[N], len[N];
+  float units[N];
+#pragma unroll
+  for (int r = 0; r < N; r++) {
+    const int i = kWave * r + lane;
+    slot[r] = i < n_rows ? (rows ? rows[i] : i) : -1;
+    if (slot[r] >= a.n_slots) slot[r] = -1;
+  }
+#pragma unroll
+  for (int r = 0; r < N; r++) len[r] = slot[r] >= 0 ? lens[slot[r]] : 0;
+  float sum = 0.0f, most = 0.0f;
+  int here = 0;
+#pragma unroll
+  for (int r = 0; r < N; r++) {
+    int tiles = len[r] > 0 ? packed_tiles(len[r], a.window) : 0;
+    if (len[r] < 0 || len[r] > a.max_len || tiles > n_ids) { len[r] = -1; tiles = 0; }
+    units[r] = len[r] > 0 ? (float)(tiles + kWindowTiles * ((len[r] - kTile * tiles + kTile - 1) / kTile)) : 0.0f;
+    sum += units[r];
+    most = fmaxf(most, units[r]);
+    here += __popcll(__builtin_amdgcn_ballot_w64(slot[r] >= 0));
+  }
+  sum = wave_sum(sum);
+  most = wave_max_dpp(most);
+  // Pieces of every context in the three shares, 10 bits each (no more than a row's one and kPlaces / 1.1 together), and up to every
+  // row in one scan; the fourth share is the longest context, one piece for each.
+  const float groups = a.groups, fair = sum * groups * a.inv_places;      // workgroups per piece; tiles for each place
+  float share[4], inv[3];
+#pragma unroll
+  for (int c = 0; c < 3; c++) {
+    share[c] = fmaxf(__builtin_ceilf(fair * kShares[c]), (float)kMinShare);
+    inv[c] = under_reciprocal(share[c]);
+  }
+  share[3] = fmaxf(most, 1.0f);
+  int cuts[N], upto[N], total = 0;
+#pragma unroll
+  for (int r = 0; r < N; r++) {
+    cuts[r] = 0;
+#pragma unroll
+    for (int c = 0; c < 3; c++) cuts[r] += (int)fmaxf(__builtin_ceilf(units[r] * inv[c]), 1.0f) << (10 * c);
+    cuts[r] = slot[r] < 0 ? 0 : cuts[r];
+    upto[r] = total + wave_scan(cuts[r]);
+    total = __builtin_amdgcn_readlane(upto[r], kWave - 1);
+  }
+  float best = INFINITY;
+  int choice = 3;
+#pragma unroll
+  for (int c = 3; c >= 0; c--) {
+    const float workgroups = (float)(c == 3 ? here : total >> (10 * c) & 1023) * groups, largest = fminf(share[c], most);
+    const float splits = c == 3 ? 1.0f : __builtin_ceilf(most * inv[c < 3 ? c : 0]);
+    const float merge = splits > 1.0f ? kMergeTiles * splits : 0.0f;
+    const float time = merge + model_time(workgroups, largest, fair, a.places, a.inv_places);
+    if (time < best) { best = time; choice = c; }
+  }
+  choice = __builtin_amdgcn_readfirstlane(choice);
+  Piece p = {};
+  p.row = -1;
+  p.total = choice == 3 ? here : total >> (10 * choice) & 1023;
+  int before = 0;
+#pragma unroll
+  for (int r = 0; r < N; r++) {
+    const uint64_t there = __builtin_amdgcn_ballot_w64(slot[r] >= 0);
+    const int n = choice == 3 ? (slot[r] >= 0 ? 1 : 0) : cuts[r] >> (10 * choice) & 1023;
+    const int up = choice == 3 ? before + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0)) + n
+                               : upto[r] >> (10 * choice) & 1023;
+    const uint64_t past = __builtin_amdgcn_ballot_w64(k < up);
+    if (p.row < 0 && past) {
+      const int l = __builtin_ctzll(past);
+      p.row = kWave * r + l;
+      p.slot = __builtin_amdgcn_readlane(slot[r], l);
+      p.len = __builtin_amdgcn_readlane(len[r], l);
+      p.splits = __builtin_amdgcn_readlane(n, l);
+      p.first = __builtin_amdgcn_readlane(up, l) - p.splits;
+      p.sp = k - p.first;
+    }
+    before += __popcll(there);
+  }
+  if (p.row < 0) return p;
+  // as plan_attention deals a context out
+  const int n = p.len < 0 ? 0 : p.len;
+  p.tiles = packed_tiles(n, a.window);
+  p.n_w = n - p.tiles * kTile;
+  const float inv_n = __builtin_amdgcn_rcpf((float)p.splits);
+  const int live = (p.n_w + kTile - 1) / kTile, each = quotient(p.tiles, p.splits, inv_n);
+  p.win_each = quotient(live, p.splits, inv_n); p.win_extra = live - p.win_each * p.splits;
+  p.win_tiles = kWindowTiles < each ? kWindowTiles : each;
+  const int dealt = p.tiles + p.win_extra * p.win_tiles;
+  p.items_q = quotient(dealt, p.splits, inv_n); p.items_r = dealt - p.items_q * p.splits;
+  return p;
+}
+
 template <int G, int NW> struct MergeLds {        // per-wave reference maximum and sum of numerators of every head
   float m[NW][G];
   float l[NW][G];
@@ -401,12 +528,9 @@ template <int G, int NW> struct MergeLds {        // per-wave reference maximum 
 // 6.97 us per launch, 8 units x 8 heads x 2000 tokens 7.35 -> 6.99, 32 units x 1 head, 3 splits 6.06 -> 5.90; all read together at
 // the start 7.24, 7.20, 6.11. Few parameters: each costs the host's launch some 15 ns.
 //
-// PAGED: a ragged batch over pages (grid: kv heads and head blocks, batch rows, splits). What the host works out for a batch of one
-// length is worked out here from the sequence's: a split is a share of 2^chunk_log2 tiles of a context, window tiles counted
-// kWindowTiles each and taken by the last one, so that a workgroup knows its first page ids before it knows the length. (Equal shares
-// of each context instead would put the length's way from memory in front of the page ids'.) The shares that a sequence does not have end at once;
-// as the slowest dimension of the grid they are dispatched behind the ones that work. The preloaded words: pointers to the
-// batch's slots, lengths and page table, entries of its rows, the share and the kv heads.
+// PAGED: a ragged batch over pages; the grid is (kv heads and head blocks, pieces of contexts), which piece is whose is found out
+// here (find_piece). From there on a piece is what a split is otherwise. The preloaded words: pointers to the batch's slots, to the
+// lengths and to the page table, the entries of its rows, the batch's rows and the kv heads.
 template <int KB, int VB, int G, int NW, bool MIXED, bool PAGED>
 __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kernel(
     const uint16_t* q, const uint32_t* packed, u32x4_t shares, u32x4_t items, u32x2_t heads, std::conditional_t<PAGED, PagedAttnArgs, AttnArgs> a) {
@@ -435,15 +559,78 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   const int h = col & (G - 1);                       // head of the column (columns past the used ones repeat them)
   const bool lo_part = !kWide<G> && col >= 8;
   const bool col_valid = (col & 7) < G;              // the column's results are stored
-  int blk = (int)blockIdx.z, jh = 0;       // block of heads; kv head (PAGED)
+  int at_blk = (int)blockIdx.z, at_sp = blockIdx.x, at_u = blockIdx.y, at_ring = blockIdx.y;
+  int jh = 0, n_kv = 0;                 // (PAGED) kv head, kv heads
+  size_t part_row = 0;                  // first row of the unit's partials
+  int n_ids = 0, tiles = 0;             // entries of a table row; packed tiles of the sequence
+  // the page ids of 64 tiles from ids_at on, a lane each (those within the piece count)
+  int ids = 0, ids_at = 0;
+  const int32_t* id_row = nullptr;      // the sequence's page ids
+  bool spoiled = false;                 // nothing that could be trusted: the results are NaN
   if constexpr (PAGED) {
-    jh = (int)blockIdx.x; blk = 0;
-    if (a.head_blocks > 1) { jh = (int)blockIdx.x / a.head_blocks; blk = (int)blockIdx.x - jh * a.head_blocks; }
+    auto word_ptr = [](uint32_t lo, uint32_t hi) { return reinterpret_cast<const int32_t*>((uint64_t)hi << 32 | lo); };
+    n_ids = (int)items[2];
+    n_kv = (int)(items[3] >> 10);
+    const int n_rows = (int)(items[3] & 1023u);
+    const int32_t* rows = word_ptr(shares[0], shares[1]);
+    const int32_t* lens = word_ptr(shares[2], shares[3]);
+    jh = (int)blockIdx.x; at_blk = 0;
+    if (a.head_blocks > 1) { jh = (int)blockIdx.x / a.head_blocks; at_blk = (int)blockIdx.x - jh * a.head_blocks; }
+    float workgroups = 0.0f;
+    if (n_rows == 1) {
+      // One sequence: shares of the size that suits max_len (the host's), so that the page ids and the length are on their way together
+      // (as a piece of a batch: one small layer 6.3 -> 7.6 us, 8 units x 2048 tokens 6.9 -> 8.2).
+      const int slot = rows ? load_uniform(rows) : 0;
+      if ((uint32_t)slot >= (uint32_t)a.n_slots) return;
+      id_row = word_ptr(items[0], items[1]) + (size_t)slot * n_ids;
+      const int n = load_uniform(lens + slot), at = (int)blockIdx.y * a.share + lane;
+      ids = at < n_ids ? id_row[at] : 0;
+      at_sp = blockIdx.y; at_u = jh; at_ring = slot * n_kv + jh;
+      tiles = n > 0 ? packed_tiles(n, a.window) : 0;
+      spoiled = n < 0 || n > a.max_len || tiles > n_ids;
+      if (spoiled) tiles = 0;
+      a.n_w = spoiled ? 0 : n - tiles * kTile;
+      const int pieces = quotient(tiles + a.share - 1, a.share, a.inv_share), live = (a.n_w + kTile - 1) / kTile;
+      a.n_splits = pieces < 1 ? 1 : pieces;
+      if ((int)blockIdx.y >= a.n_splits) return;
+      a.win_each = quotient(live, a.n_splits, __builtin_amdgcn_rcpf((float)a.n_splits)); a.win_extra = live - a.win_each * a.n_splits;
+      a.items_q = a.share; a.items_r = 0; a.win_tiles = 0;
+      part_row = (size_t)jh * a.n_splits;
+      workgroups = (float)a.n_splits * a.groups;
+    } else {
+      __shared__ Piece s_piece;
+      if (wave == 0) {
+        const Piece p = n_rows <= kWave ? find_piece<1>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
+                                        : find_piece<kBatchRows / kWave>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane);
+        if (lane == 0) s_piece = p;
+      }
+      lds_barrier();
+      Piece piece;
+      {
+        constexpr int kWords = sizeof(Piece) / 4;
+        int w[kWords];
+#pragma unroll
+        for (int i = 0; i < kWords; i++) w[i] = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(&s_piece)[i]);
+        __builtin_memcpy(&piece, w, sizeof(Piece));
+      }
+      if (piece.row < 0) return;
+      at_sp = piece.sp;
+      at_u = piece.row * n_kv + jh;
+      at_ring = piece.slot * n_kv + jh;
+      part_row = (size_t)piece.first * n_kv + (size_t)jh * piece.splits;
+      spoiled = piece.len < 0;
+      id_row = word_ptr(items[0], items[1]) + (size_t)piece.slot * n_ids;
+      tiles = piece.tiles;
+      a.n_splits = piece.splits;
+      a.n_w = piece.n_w;
+      a.win_each = piece.win_each; a.win_extra = piece.win_extra; a.win_tiles = piece.win_tiles;
+      a.items_q = piece.items_q; a.items_r = piece.items_r;
+      workgroups = (float)piece.total * a.groups;
+    }
+    a.w0_tile = ring_tile(tiles, a.ring_tiles, a.ring_magic);
+    a.even = workgroups > 0.5f * a.places && workgroups <= a.places;
   }
-  const int sp = PAGED ? blockIdx.z : blockIdx.x;
-  int u = blockIdx.y;
-  const int n_kv = PAGED ? (int)(items[3] >> 8) : 0;
-  if constexpr (PAGED) u = (int)blockIdx.y * n_kv + jh;
+  const int blk = at_blk, sp = at_sp, u = at_u, uw = at_ring;      // block of heads; split; unit: of q and out, and of the rings
   // Query groups of more than 8 heads run as blocks of 8 or 16 heads in workgroups of their own (grid z): the blocks
   // of a unit read the same records and window rows at about the same time, so a tile comes from HBM once and from
   // the caches after that. uo numbers the (unit, head block) pairs; blocks of 8: rows uo*8 .. uo*8+7 of q and out.
@@ -464,21 +651,11 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   int first = sp * a.items_q + (sp < a.items_r ? sp : a.items_r) - extra * a.win_tiles;
   int last = first + a.items_q + (sp < a.items_r ? 1 : 0) - (sp < a.win_extra ? a.win_tiles : 0);
   int wins = a.win_each + (sp < a.win_extra ? 1 : 0);
-  // PAGED: the slot and, as soon as it is known, the length and the page ids of the share's first 64 tiles (a lane each)
-  int slot = 0, n_tok = 0, ids = 0, ids_at = 0;
-  const int32_t* id_row = nullptr;
-  int n_ids = 0;                        // entries of a table row
-  bool spoiled = false;                 // nothing that could be trusted: the results are NaN
-  auto word_ptr = [](uint32_t lo, uint32_t hi) { return reinterpret_cast<const int32_t*>((uint64_t)hi << 32 | lo); };
-  auto load_ids = [&](int from) {      // page ids of the tiles from `from` on (a lane each, those within the table's row)
-    const int i = from + lane;
-    return i < n_ids ? id_row[i] : 0;
-  };
+  auto load_ids = [&]() { return ids_at + lane < last ? id_row[ids_at + lane] : 0; };
   if constexpr (PAGED) {
-    const int32_t* rows = word_ptr(shares[0], shares[1]);
-    slot = rows ? load_uniform(rows + blockIdx.y) : (int)blockIdx.y;
-    n_ids = (int)items[2];
-    first = sp << (items[3] & 255u);
+    if (last > tiles) last = tiles;                // (the last share of one sequence)
+    ids_at = first;
+    if ((items[3] & 1023u) != 1u) ids = load_ids();
   }
 
   // ---- the query and the wave's first tile are requested before anything else is done.
@@ -491,7 +668,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   // loaded by the hi columns in use only (a load's cost at the start of a launch is its active lanes), copied to the lo columns later;
   // groups of 1 or 2 heads use it for window tiles only, and the other waves' requests are better spent on their first tiles (16 layers of
   // 256 units: 356.4 us with, 352.9 us without)
-  const bool needs_q = MIXED || PAGED || G > 2 || wave < a.win_each + (sp < a.win_extra ? 1 : 0);
+  const bool needs_q = MIXED || G > 2 || wave < a.win_each + (sp < a.win_extra ? 1 : 0);
 #pragma unroll
   for (int ks = 0; ks < 4; ks++) {
     qB[ks] = half8_t{0, 0, 0, 0, 0, 0, 0, 0};
@@ -511,35 +688,15 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   for (int hh = 0; hh < G; hh++) qraw[hh] = kOwnOperand<G> || kLateQuery ? 0u : reinterpret_cast<const uint32_t*>(qbase + hh * kD)[lane];
 
   constexpr uint32_t kRecBytes = (uint32_t)(record_words(KB, VB) * 4);
-  if constexpr (PAGED) {
-    if ((uint32_t)slot >= (uint32_t)a.n_slots) return;             // padding
-    id_row = word_ptr(items[0], items[1]) + (size_t)slot * n_ids;
-    n_tok = load_uniform(word_ptr(shares[2], shares[3]) + slot);
-    ids = load_ids(first);
-    ids_at = first;
-    int tiles = n_tok > 0 ? packed_tiles(n_tok, a.window) : 0;
-    a.n_w = n_tok - tiles * kTile;
-    wins = (a.n_w + kTile - 1) / kTile;
-    const int log2 = (int)(items[3] & 255u), share = 1 << log2, win_share = kWindowTiles * wins < share ? kWindowTiles * wins : share;
-    a.n_splits = (tiles + win_share + share - 1) >> log2;
-    if (a.n_splits < 1) a.n_splits = 1;
-    if (n_tok < 0 || n_tok > a.max_len || tiles > n_ids || a.n_splits > a.max_splits) { spoiled = true; tiles = 0; a.n_w = 0; wins = 0; a.n_splits = 1; }
-    if (sp >= a.n_splits) return;
-    if (sp < a.n_splits - 1) wins = 0;
-    a.w0_tile = ring_tile(tiles, a.ring_tiles, a.ring_magic);
-    last = first + share < tiles ? first + share : tiles;
-    if (first > last) first = last;
-  }
   int n_pages = 0;
   if constexpr (PAGED) n_pages = a.n_pages;
-  // (lanes past the share's tiles count for nothing)
   auto check_ids = [&](int& x) {
     const bool bad = (uint32_t)x >= (uint32_t)n_pages;
     spoiled |= __any(bad && ids_at + lane < last) != 0;
     x = bad ? 0 : x;
   };
   // (4 heads with 3-bit Keys and 3- or 4-bit Values have no register for the ids around the loop: in LDS, a copy for each wave)
-  constexpr bool kIdsInLds = PAGED && G == 4 && KB == 3 && VB >= 3;
+  constexpr bool kIdsInLds = PAGED && KB == 3 && ((G == 4 && VB >= 3) || (G == 8 && VB == 2));
   __shared__ int s_ids[kIdsInLds ? kWaves : 1][kIdsInLds ? kWave : 1];
   auto keep_ids = [&]() {
     check_ids(ids);
@@ -552,15 +709,14 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   };
   if constexpr (PAGED) keep_ids();
   const int p_begin = first, p_end = last, n_win = wins;
-  const int uw = PAGED ? slot * n_kv + jh : u;                     // of the rings
   const rsrc_t up = make_rsrc(reinterpret_cast<const char*>(a.packed) + (size_t)u * a.tiles_cap * kRecBytes, (uint32_t)a.tiles_cap * kRecBytes);
   // tile t (wave-uniform, the wave's tiles come in ascending order), past the end the last one
   auto load_tile = [&](Stage<KB, VB>& st, int t, uint32_t l16) {
     if constexpr (PAGED) {
       if (t >= p_end) t = p_end - 1;
-      if (t - ids_at >= kWave) {       // (only shares of more than 64 tiles: contexts past 2 M tokens)
+      if (t - ids_at >= kWave) {
         ids_at = t;
-        ids = load_ids(t);
+        ids = load_ids();
         keep_ids();
       }
       int id;
@@ -898,8 +1054,8 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   // ring slot of tile j between the fronts
   auto mixed_slot = [&](int j) { int wi = a.m_ring + j; wi = wi >= a.ring_tiles ? wi - a.ring_tiles : wi; return wi * kTile; };
   if (!early) {
-    int r = PAGED ? wave : sp + wave * a.n_splits;       // < the number of live tiles, since wave < n_win
-    const int r_step = PAGED ? kWaves : kWaves * a.n_splits;
+    int r = sp + wave * a.n_splits;                      // < the number of live tiles, since wave < n_win
+    const int r_step = kWaves * a.n_splits;
     int left = (n_win - wave + kWaves - 1) / kWaves;     // tiles of this wave
     for (int begin = 1; left > 0; left--, r += r_step) {
       asm volatile("" : "+s"(begin));     // (keeps the first pass from being compiled a second time: the code is read cold at the start of a launch)
@@ -1442,7 +1598,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     // and 17.7; at 126 tiles the same within 1 %. The level from the number of the claimed tile alone, several steps at once: 17.6 and
     // 18.3.)
     int prio = 0, next_at = p_end;
-    if constexpr (kWaves == 8 && !PAGED) {
+    if constexpr (kWaves == 8) {
       if (a.even && p_end - p_begin > 12) {      // (a handful of tiles, 32 units of 8: 6.2 us without, 6.4 with)
         prio = 3;
         next_at = p_begin + ((p_end - p_begin) >> 1);
@@ -1451,7 +1607,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     }
     while (it < p_end) {
       const int ticket = grab_issue();
-      if constexpr (kWaves == 8 && !PAGED) {
+      if constexpr (kWaves == 8) {
         if (it >= next_at) {
           prio--;
           next_at = prio > 0 ? it + ((p_end - it) >> 1) : p_end;
@@ -1464,7 +1620,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
       it = grab_take(ticket);
       load_tile(st, it, lane16);
     }
-    if constexpr (kWaves == 8 && !PAGED) __builtin_amdgcn_s_setprio(0);
+    if constexpr (kWaves == 8) __builtin_amdgcn_s_setprio(0);
   }
 
   {
@@ -1540,9 +1696,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   };
   uint16_t* outp = a.out + row0 * kD;
   // partial of split s, head hh of the block: [unit][block][split][head of the block] (blocks of 16: [unit][split][head of the group])
-  int part_rows = a.n_splits;
-  if constexpr (PAGED) part_rows = a.max_splits;
-  const size_t part0 = kWide<G> ? (size_t)u * part_rows * a.G + head0 : (size_t)uo * part_rows * G;
+  const size_t part0 = PAGED ? part_row * a.G + head0 : kWide<G> ? (size_t)u * a.n_splits * a.G + head0 : (size_t)uo * a.n_splits * G;
   const int part_step = kWide<G> ? a.G : G;
   auto part_at = [&](int s, int hh) { return a.part + (part0 + (size_t)s * part_step + hh) * (kD + 2); };
   auto put_out = [&](int hh, const float2_t& O, float Lsum) {
@@ -1836,15 +1990,15 @@ hipError_t launch_decode_attn<kNW, kMixed>(const AttnArgs& a, int k_bits, int v_
   return hipErrorInvalidValue;
 }
 #else
-hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int chunk_log2, int k_bits, int v_bits, int block, int B, hipStream_t s) {
-  const dim3 grid(a.Hkv * a.head_blocks, B, a.max_splits);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s) {
+  const dim3 grid(a.Hkv * a.head_blocks, pieces);
   auto words = [](const int32_t* x, const int32_t* y) {
     const uint64_t p = reinterpret_cast<uint64_t>(x), q = reinterpret_cast<uint64_t>(y);
     return u32x4_t{(uint32_t)p, (uint32_t)(p >> 32), (uint32_t)q, (uint32_t)(q >> 32)};
   };
   const u32x4_t shares = words(rows, pages.lens);
   u32x4_t items = words(pages.table, nullptr);
-  items[2] = (uint32_t)pages.max_tiles; items[3] = (uint32_t)chunk_log2 | (uint32_t)a.Hkv << 8;
+  items[2] = (uint32_t)pages.max_tiles; items[3] = (uint32_t)n_rows | (uint32_t)a.Hkv << 10;
   switch (k_bits * 10 + v_bits) {
     case 11: return launch_g<1, 1>(a, shares, items, block, grid, s);
     case 12: return launch_g<1, 2>(a, shares, items, block, grid, s);

@@ -13,7 +13,7 @@ int check_pages(const kvmix_pages* p) {
   if (!p || !p->table || !p->lens || !p->grown || !p->refs || !p->used || !p->status) return KVMIX_ERR_NULL;
   if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->grown) || !aligned4(p->refs) || !aligned4(p->used) || !aligned4(p->status)) return KVMIX_ERR_ALIGN;
   // (page counts to 4 M: the grow kernel keeps one of 1024 counters for every 4096)
-  if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages > (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 26)) return KVMIX_ERR_BAD_SHAPE;
+  if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages > (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 23)) return KVMIX_ERR_BAD_SHAPE;
   if (p->window < 0 || p->window % kTile) return KVMIX_ERR_BAD_SHAPE;
   return KVMIX_OK;
 }
@@ -42,25 +42,42 @@ int check_together(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const kvmi
 
 uint32_t ring_magic(int ring_tiles) { return ring_tiles == 1 ? 0u : (uint32_t)((1ULL << 32) / (uint32_t)ring_tiles + 1); }
 
-// How a ragged launch shares out contexts of up to max_len tokens.
-struct PagedPlan { int block, head_blocks, log2, splits; size_t counters, bytes; };
+// A ragged launch: batch rows in launches of at most kRows, each with a workgroup per piece of a context, kv head and block of heads.
+// Pieces are made on the device (find_piece in kvmix_attn.hip): from the tiles of the whole batch a share for each of the kPlaces
+// workgroups that the chip holds at once (8 waves, two to a compute unit), so that there are at most kPlaces / (kv heads x head blocks)
+// pieces and one more for every row.
+constexpr int kRows = 512, kCus = 256, kPlaces = 2 * kCus;
+struct PagedPlan { int block, head_blocks, rows, pieces, share; size_t counters, bytes; };
 PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits) {
   PagedPlan p;
-  const int G = sh->Hq / sh->Hkv, units = sh->B * sh->Hkv;
+  const int G = sh->Hq / sh->Hkv;
+  // 8 heads with 3- or 4-bit Values do not fit the registers of 8 waves as a block of 8: half a block of 16 (see plan_attention)
   p.block = G <= 4 || (G == 8 && v_bits < 3) ? G : 16;
   p.head_blocks = (G + p.block - 1) / p.block;
-  const int tiles = packed_tiles(max_len, window), held = max_len < window + kTile ? max_len : window + kTile - 1;
-  const int win = 3 * ((held + kTile - 1) / kTile);
-  const long long work = (long long)units * p.head_blocks * (tiles + win);
-  for (p.log2 = 3; p.log2 < 6 && (long long)512 << p.log2 < work; p.log2++) {}
-  auto count = [&]() {
-    const int share = 1 << p.log2;
-    return (int)(((long long)tiles + (win < share ? win : share) + share - 1) >> p.log2);
-  };
-  while (count() > 1024) p.log2++;
-  p.splits = count() < 1 ? 1 : count();
-  p.counters = ((size_t)units * (G > 8 ? G / 8 : 1) * 4 + 255) / 256 * 256;
-  p.bytes = p.counters + (size_t)units * p.splits * G * (kD + 2) * sizeof(float);
+  p.rows = sh->B < kRows ? sh->B : kRows;
+  const int tiles = packed_tiles(max_len, window), held = max_len - window < kTile ? max_len : window + kTile - 1;
+  const long long most = tiles + (long long)kWindowTiles * (((long long)held + kTile - 1) / kTile), each = most <= kMinShare ? 1 : (most + kMinShare - 1) / kMinShare;
+  const long long by_places = p.rows + kPlaces / (sh->Hkv * p.head_blocks) + 1, by_length = p.rows * each;
+  p.pieces = (int)(by_places < by_length ? by_places : by_length);
+  p.counters = ((size_t)p.rows * sh->Hkv * (G > 8 ? G / 8 : 1) * 4 + 255) / 256 * 256;
+  p.bytes = p.counters + (size_t)p.pieces * sh->Hkv * G * (kD + 2) * sizeof(float);
+  p.share = 1;
+  if (sh->B == 1) {
+    // (one sequence: the share that suits max_len, chosen as the device chooses a batch's)
+    const int groups = sh->Hkv * p.head_blocks;
+    const float fair = (float)most * groups / kPlaces;
+    float best = INFINITY;
+    int splits = 1;
+    for (int c = 3; c >= 0; c--) {
+      const float share = c == 3 ? (float)most : std::fmax(std::ceil(fair * kShares[c]), (float)kMinShare);
+      const float n = c == 3 ? 1.0f : std::fmax(std::ceil((float)most / share), 1.0f);
+      const float time = (n > 1.0f ? kMergeTiles * n : 0.0f) + model_time(n * groups, std::fmin(share, (float)most), fair, kPlaces, 1.0f / kPlaces);
+      if (time < best) { best = time; splits = (int)n; }
+    }
+    if (splits > p.pieces) splits = p.pieces;
+    p.share = tiles > splits ? (tiles + splits - 1) / splits : 1;
+    p.pieces = tiles > 0 ? (tiles + p.share - 1) / p.share : 1;
+  }
   return p;
 }
 
@@ -191,12 +208,11 @@ int kvmix_paged_workspace_bytes(const kvmix_shape* sh, int max_len, size_t* byte
   if (st) return st;
   if (!bytes) return KVMIX_ERR_NULL;
   if (max_len < 1) return KVMIX_ERR_BAD_SHAPE;
-  // any window and any widths: the most splits over both (a window packs fewer tiles; its own are at most one share more)
+  // (any window and any widths: a token counts for more in a window than in a page, so that one which holds everything has the most pieces)
   *bytes = 0;
   for (int v_bits = 2; v_bits <= 3; v_bits++) {
-    PagedPlan p = plan_paged(sh, 0, max_len, v_bits);
-    const size_t more = p.bytes + (size_t)sh->B * sh->Hkv * 2 * (sh->Hq / sh->Hkv) * (kD + 2) * sizeof(float);
-    if (more > *bytes) *bytes = more;
+    const PagedPlan p = plan_paged(sh, max_len / kTile * kTile, max_len, v_bits);
+    if (p.bytes > *bytes) *bytes = p.bytes;
   }
   return KVMIX_OK;
 }
@@ -219,29 +235,39 @@ int kvmix_paged_decode_attn(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, c
   const long long most = (long long)p->max_tiles * kTile + p->window + kTile - 1;
   if (max_len <= 0 || max_len > most) max_len = most < 0x7fffffffLL ? (int)most : 0x7fffffff;
   const PagedPlan plan = plan_paged(sh, p->window, max_len, cfg->v_bits);
+  const int G = sh->Hq / sh->Hkv;
   PagedAttnArgs a{};
-  if (plan.splits > 1) {
+  if (plan.pieces > plan.rows) {
     if (!workspace) return KVMIX_ERR_NULL;
     if (!aligned16(workspace)) return KVMIX_ERR_ALIGN;
     if (workspace_bytes < plan.bytes) return KVMIX_ERR_WORKSPACE;
     a.counters = reinterpret_cast<uint32_t*>(workspace);
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + plan.counters);
   }
-  const int G = sh->Hq / sh->Hkv, counted = sh->B * sh->Hkv * (G > 8 ? G / 8 : 1);
+  const int counted = plan.rows * sh->Hkv * (G > 8 ? G / 8 : 1);
   a.counter_stride = 1;
   while (a.counter_stride * 2 * counted <= 64) a.counter_stride *= 2;
-  a.q = q; a.out = out; a.G = G;
+  a.G = G;
   a.packed = c->pool;
   a.k_win = c->k_win; a.v_win = c->v_win;
   a.W_cap = c->W_cap; a.ring_tiles = c->W_cap / kTile;
   a.head_blocks = plan.head_blocks;
-  a.max_splits = plan.splits;
   a.n_slots = p->n_slots; a.n_pages = p->n_pages; a.Hkv = sh->Hkv; a.window = p->window; a.max_len = max_len;
+  a.groups = (float)(sh->Hkv * plan.head_blocks);
+  a.places = (float)kPlaces; a.inv_places = 1.0f / (float)kPlaces;
+  a.share = plan.share; a.inv_share = 1.0f / (float)plan.share;
   a.ring_magic = ring_magic(a.ring_tiles);
   const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)kD);
   a.scale_log2 = scale * 1.4426950408889634f;
-  const hipError_t e = launch_paged_attn(a, *p, rows, plan.log2, cfg->k_bits, cfg->v_bits, plan.block, sh->B, (hipStream_t)stream);
-  return e == hipSuccess ? KVMIX_OK : hip_fail(e);
+  for (int b = 0; b < sh->B; b += kRows) {
+    const int n = sh->B - b < kRows ? sh->B - b : kRows;
+    a.q = q + (size_t)b * sh->Hq * kD; a.out = out + (size_t)b * sh->Hq * kD;
+    kvmix_pages here = *p;
+    if (!rows) { here.table += (size_t)b * p->max_tiles; here.lens += b; a.k_win = c->k_win + (size_t)b * sh->Hkv * c->W_cap * kD; a.v_win = c->v_win + (size_t)b * sh->Hkv * c->W_cap * kD; a.n_slots = p->n_slots - b; }
+    const hipError_t e = launch_paged_attn(a, here, rows ? rows + b : nullptr, n, plan.pieces, cfg->k_bits, cfg->v_bits, plan.block, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e);
+  }
+  return KVMIX_OK;
 }
 
 int kvmix_rope_frequencies(int rotary_dim, double base, int scaling, double factor, int original_len, double low, double high, float* frequencies,

@@ -18,15 +18,16 @@ hipError_t launch_pages_free(const kvmix_pages&, const int32_t*, int, hipStream_
 hipError_t launch_pages_fork(const kvmix_pages&, const int32_t*, const int32_t*, int, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_pages_compact(const kvmix_pages&, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_copy(const CopyArgs&, hipStream_t) { return hipErrorUnknown; }
-long long seen[4];
-hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages&, const int32_t*, int log2, int, int, int block, int, hipStream_t) {
-  seen[0] = a.max_splits; seen[1] = log2; seen[2] = block;
+long long seen[5];
+hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages&, const int32_t*, int n_rows, int pieces, int, int, int block, hipStream_t) {
+  seen[0] = pieces; seen[1] = n_rows; seen[2] = block;
+  seen[4] = a.share;
   seen[3] = a.part ? reinterpret_cast<char*>(a.part) - reinterpret_cast<char*>(a.counters) : 0;
   return hipSuccess;
 }
 }  // namespace kvmix
 
-// One call; taken: splits, log2 of the share, heads per block, bytes of counters
+// One call; taken, of its last launch: pieces, batch rows, heads per block, bytes of counters, tiles of a share of one sequence
 extern "C" int paged_plan(int B, int Hkv, int G, int v_bits, int W, int max_len, size_t workspace_bytes, long long* taken) {
   const kvmix_shape sh{B, Hkv * G, Hkv, kD, kTile};
   const kvmix_layer_cfg cfg{2, v_bits, W};
@@ -35,6 +36,6 @@ extern "C" int paged_plan(int B, int Hkv, int G, int v_bits, int W, int max_len,
   const kvmix_paged_cache c{reinterpret_cast<uint32_t*>(p), p, p, 100, B, W + kTile};
   const kvmix_pages pages{i, i, i, i, reinterpret_cast<uint32_t*>(i), i, i, B, 100, 1 << 20, W};
   const int st = kvmix_paged_decode_attn(&sh, &cfg, p, &c, &pages, i, max_len, 0.0f, p, workspace_bytes ? p : nullptr, workspace_bytes, nullptr);
-  for (int k = 0; k < 4; k++) taken[k] = seen[k];
+  for (int k = 0; k < 5; k++) taken[k] = seen[k];
   return st;
 }

@@ -31,7 +31,7 @@ def cache(**change):
 
 BAD_PAGES = [(dict(table=None), -1), (dict(lens=None), -1), (dict(grown=None), -1), (dict(refs=None), -1), (dict(used=None), -1), (dict(status=None), -1),
              (dict(table=A + 2), -5), (dict(status=A + 1), -5), (dict(n_slots=0), -4), (dict(n_pages=0), -4), (dict(n_pages=(1 << 22) + 1), -4),
-             (dict(max_tiles=0), -4), (dict(max_tiles=(1 << 26) + 1), -4), (dict(window=-1), -4), (dict(window=40), -4)]
+             (dict(max_tiles=0), -4), (dict(max_tiles=(1 << 23) + 1), -4), (dict(window=-1), -4), (dict(window=40), -4)]
 
 
 @pytest.mark.parametrize("change,status", BAD_PAGES)
@@ -102,8 +102,8 @@ def test_counts_and_pointers(kv):
 
 @pytest.fixture(scope="module")
 def plan(tmp_path_factory):
-    """kvmix_paged_decode_attn with its launch taken down: (B, Hkv, G, v_bits, W, max_len, workspace) -> status, splits, log2 of the share, heads per
-    block, bytes of counters."""
+    """kvmix_paged_decode_attn with its launch taken down: (B, Hkv, G, v_bits, W, max_len, workspace) -> status and, of the last
+    launch, pieces, batch rows, heads per block, bytes of counters, tiles of a share of one sequence."""
     import os
     import subprocess
     from paper_2506_08018_amd import build
@@ -114,27 +114,51 @@ def plan(tmp_path_factory):
     f.argtypes = [C.c_int] * 6 + [C.c_size_t, C.c_void_p]
 
     def run(*args):
-        out = (C.c_longlong * 4)()
+        out = (C.c_longlong * 5)()
         return (f(*args, out), *out)
 
     return run
 
 
+def packed(n, W):
+    return 0 if n < W + 32 else (n - W) // 32
+
+
 def test_workspace_is_enough_for_every_window_and_width(kv, plan):
-    for B, Hkv, G in [(1, 1, 1), (1, 8, 4), (3, 2, 8), (16, 8, 4), (64, 8, 8), (2, 1, 72), (200, 32, 1)]:
+    for B, Hkv, G in [(1, 1, 1), (1, 8, 4), (3, 2, 8), (16, 8, 4), (64, 8, 8), (2, 1, 72), (700, 32, 1), (1000, 64, 8)]:
         for n in (1, 40, 300, 1000, 5000, 40000, 300000, 2 ** 31 - 1):
             need = kv.paged_workspace_bytes(kv.Shape(B, G * Hkv, Hkv), n)
             for W in (0, 32, 64, 256, 4096):
                 for vb in (2, 3):
                     for m in {n, max(1, n // 2), max(1, n - 33)}:
-                        st, splits, log2, block, counters = plan(B, Hkv, G, vb, W, m, need)
+                        st, pieces, rows, block, counters, _ = plan(B, Hkv, G, vb, W, m, need)
                         assert st == 0, (B, Hkv, G, n, W, vb, m)
-                        m = min(m, 32 * (1 << 20) + W + 31)                            # a table row holds no more
-                        tiles = 0 if m < W + 32 else (m - W) // 32
-                        held = min(m, W + 31)
-                        # what the kernel works out for the longest sequence
-                        assert splits >= max(1, (tiles + min(3 * ((held + 31) // 32), 1 << log2) + (1 << log2) - 1) >> log2)
-                        assert splits <= 1024 and (splits == 1 or counters + B * Hkv * splits * G * 520 <= need)
+                        assert pieces <= min(B, 512) or counters + pieces * Hkv * G * 520 <= need
+
+
+def pieces_of(lens, W, places_scale, share):
+    """What the kernel works out (find_piece) with the smallest share that it may take, in its arithmetic: fp32; of one sequence by the host's share."""
+    if len(lens) == 1:
+        return max(1, -(-packed(lens[0], W) // share))
+    units = np.array([0 if n <= 0 else packed(n, W) + 3 * -(-(n - 32 * packed(n, W)) // 32) for n in lens], np.int64)
+    size = int(np.ceil(np.float32(units.astype(np.float32).sum(dtype=np.float32)) * np.float32(places_scale)))
+    share = max(8, size)
+    return int(np.maximum(1, -(-units // share)).sum())
+
+
+def test_the_grid_holds_every_piece(kv, plan):
+    """However the lengths are spread below max_len, the pieces that they make are no more than the launch has workgroups for."""
+    rng = np.random.default_rng(1)
+    for B, Hkv, G in [(1, 1, 1), (1, 8, 4), (2, 16, 1), (5, 2, 16), (64, 8, 8), (300, 1, 4), (512, 32, 1), (2, 1, 72), (7, 600, 1)]:
+        for max_len in (1, 33, 95, 300, 5000, 70000, 2000000):
+            for W in (0, 32, 256):
+                need = kv.paged_workspace_bytes(kv.Shape(B, G * Hkv, Hkv), max_len)
+                st, pieces, rows, block, _, share = plan(B, Hkv, G, 2, W, max_len, need)
+                assert st == 0 and rows == B
+                HH = Hkv * -(-G // block)
+                for lens in ([max_len] * B, [max_len] + [0] * (B - 1), [max_len] + [1] * (B - 1), rng.integers(0, max_len + 1, B).tolist(),
+                             np.exp(rng.uniform(0, np.log(max_len + 1), B)).astype(int).tolist(), [max(0, max_len - 31)] * B):
+                    assert pieces_of(lens, W, HH / 512, share) <= pieces, (B, Hkv, G, max_len, W, lens[:8])
 
 
 def test_rotation_refusals(kv):
