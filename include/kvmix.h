@@ -393,24 +393,25 @@ int kvmix_rope_frequencies(int rotary_dim, double base, int scaling, double fact
                            float* frequencies, float* amplitude);
 
 typedef struct {
+  const void* in;            /* element (i, h, d) at i*token_stride + h*head_stride + d (elements; multiples of 16 bytes; any sign or zero) */
+  uint16_t* out;             /* [n_tokens][heads][128], contiguous */
+  int64_t token_stride, head_stride;
+} kvmix_rope_side;           /* in and out NULL: left out */
+typedef struct {
   const float* frequencies;  /* device, [rotary_dim / 2]: radians per position (NULL with rotary_dim 0) */
   int32_t rotary_dim;        /* channels 0 .. rotary_dim - 1 of a head are rotated: a multiple of 16, 0 to 128 */
   int32_t interleaved;       /* pairs (2i, 2i + 1); 0: (i, i + rotary_dim / 2) */
   float amplitude;           /* of cosine and sine */
   float eps;                 /* of the norms */
-  const void* q_weight;      /* device, [128] of the inputs' type, 16-byte aligned: x / sqrt(mean(x^2) + eps) * weight over the 128 channels ahead */
-  const void* k_weight;      /* of the rotation; NULL: no norm for that side */
-} kvmix_rope;
+  const void* q_weight;      /* device, [128] of the inputs' type: x / sqrt(mean(x^2) + eps) * weight over the 128 channels ahead of the rotation; */
+  const void* k_weight;      /* NULL: no norm for that side */
+  kvmix_rope_side q, k, v;   /* Hq, Hkv and Hkv heads */
+} kvmix_rope;                /* host memory; every device pointer 16-byte aligned */
 /* Queries and Keys of n_tokens tokens as the projections leave them, normed and rotated by positions[i], and Values, as the fp16 that the cache
- * and the attention take: out[i][head][128] for q (Hq heads), k, v (Hkv heads), contiguous. Inputs of one type (kvmix_dtype), element
- * (i, h, d) of each at i*token_stride + h*head_stride + d with strides of their own (elements; multiples of 16 bytes; any sign or zero);
- * pointers 16-byte aligned. Any of the three may be left out (input and output NULL). Angles are taken in binary64, everything else in
- * fp32 with one rounding at the end; positions are any int32. Outputs may be the inputs' memory only where the layout is the same, element for
- * element. One launch. */
-int kvmix_qk_norm_rope(const kvmix_shape* shape, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions,
-                       const void* q, int64_t q_token_stride, int64_t q_head_stride, uint16_t* q_out,
-                       const void* k, int64_t k_token_stride, int64_t k_head_stride, uint16_t* k_out,
-                       const void* v, int64_t v_token_stride, int64_t v_head_stride, uint16_t* v_out, void* stream);
+ * and the attention take. Inputs of one type (kvmix_dtype). Angles are taken in binary64, everything else in fp32 with one rounding
+ * at the end (|x| < 10^18 with a norm: the sum of squares is an fp32 number); positions (4-byte aligned) are any int32. An output may be its input's
+ * memory where the layout is the same, element for element. One launch. */
+int kvmix_qk_norm_rope(const kvmix_shape* shape, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,7 @@
 """ctypes marshalling for include/kvmix.h. No arithmetic of the method lives here."""
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libkvmix.so")
@@ -77,7 +78,7 @@ def lib():
                            ("kvmix_paged_append", [P, P] + [P, I64, I64] * 2 + [P] * 4 + [I, P]), ("kvmix_paged_workspace_bytes", [P, I, P]),
                            ("kvmix_paged_decode_attn", [P] * 6 + [I, C.c_float, P, P, SZ, P]),
                            ("kvmix_rope_frequencies", [I, C.c_double, I, C.c_double, I, C.c_double, C.c_double, P, P]),
-                           ("kvmix_qk_norm_rope", [P, P, I, I, P] + [P, I64, I64, P] * 3 + [P])):
+                           ("kvmix_qk_norm_rope", [P, P, I, I, P, P])):
             getattr(L, name).restype = I
             getattr(L, name).argtypes = args
         L.kvmix_dequant.restype = I
@@ -258,17 +259,25 @@ class _PagedCacheStruct(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pool", "k_win", "v_win")] + [(n, C.c_int32) for n in ("n_pages", "n_slots", "W_cap")]
 
 
-class _RopeStruct(C.Structure):
-    _fields_ = [("frequencies", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float), ("eps", C.c_float),
-                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+# Host time per call, a launch included, is as long as the smaller kernels: tensors are asked for as little as their checks need, structures that a
+# program keeps have their reference made once (one token of qk_norm_rope 9.7 -> 5.9 us a pass, paged_append 6.1 -> 5.2).
+_types = None
+
+
+def _torch_types():
+    """(int32, fp16, fp32, {type: kvmix_dtype}) of torch, which is imported when it is first needed."""
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.int32, torch.float16, torch.float32, {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
+    return _types
 
 
 def _int32(t, n, what):
-    """Device address of a contiguous int32 tensor of at least n elements (n None: any); None stays None."""
+    """Device address of a contiguous int32 tensor of at least n elements; None stays None."""
     if t is None:
         return None
-    assert t.element_size() == 4 and not t.is_floating_point() and t.is_contiguous(), f"{what}: contiguous int32 expected"
-    assert n is None or t.numel() >= n, f"{what}: {t.numel()} elements, {n} expected"
+    assert t.dtype is (_types or _torch_types())[0] and t.is_contiguous() and t.numel() >= n, f"{what}: contiguous int32, {n} elements at least"
     return t.data_ptr()
 
 
@@ -292,13 +301,14 @@ class Pages:
         assert not given, f"unknown buffers {sorted(given)}"
         self.c = _PagesStruct(*[_int32(getattr(self, name), n, name) for name, n in sizes.items()], _int32(self.moves, 4 + 3 * n_pages, "moves"),
                               n_slots, n_pages, max_tiles, window)
+        self.ref = C.byref(self.c)
 
     def _with_moves(self):
         if self.moves is None:
             import torch
             self.moves = torch.zeros(4 + 3 * self.n_pages, dtype=torch.int32, device=self.device)
             self.c.moves = self.moves.data_ptr()
-        return C.byref(self.c)
+        return self.ref
 
 
 class PagedCache:
@@ -318,23 +328,24 @@ class PagedCache:
             setattr(self, name, t)
         self.n_pages, self.n_slots, self.W_cap = n_pages, n_slots, W_cap
         self.c = _PagedCacheStruct(*[None if t is None else t.data_ptr() for t in (self.pool, self.k_win, self.v_win)], n_pages, n_slots, W_cap)
+        self.ref = C.byref(self.c)
 
 
 def pages_grow(pages, rows=None, cu=None, n_rows=None, stream=None):
     """Rows (slots; None: row b is slot b) get room for cu[b + 1] - cu[b] more tokens each (None: one)."""
     n = n_rows if n_rows is not None else rows.numel() if rows is not None else cu.numel() - 1
-    _check(lib().kvmix_pages_grow(C.byref(pages.c), _int32(rows, n, "rows"), _int32(cu, n + 1, "cu"), n, _stream(stream)), "kvmix_pages_grow")
+    _check(lib().kvmix_pages_grow(pages.ref, _int32(rows, n, "rows"), _int32(cu, n + 1, "cu"), n, _stream(stream)), "kvmix_pages_grow")
 
 
 def pages_free(pages, rows, stream=None):
     """The slots in `rows` are empty again, pages that nobody else holds are free."""
-    _check(lib().kvmix_pages_free(C.byref(pages.c), _int32(rows, None, "rows"), rows.numel(), _stream(stream)), "kvmix_pages_free")
+    _check(lib().kvmix_pages_free(pages.ref, _int32(rows, 0, "rows"), rows.numel(), _stream(stream)), "kvmix_pages_free")
 
 
 def pages_fork(pages, src, dst, stream=None):
     """Slot dst[i], empty, becomes a second holder of the pages of src[i] (rings: copy_windows, per layer)."""
     n = src.numel()
-    _check(lib().kvmix_pages_fork(C.byref(pages.c), _int32(src, n, "src"), _int32(dst, n, "dst"), n, _stream(stream)), "kvmix_pages_fork")
+    _check(lib().kvmix_pages_fork(pages.ref, _int32(src, n, "src"), _int32(dst, n, "dst"), n, _stream(stream)), "kvmix_pages_fork")
 
 
 def pages_compact(pages, stream=None):
@@ -344,13 +355,13 @@ def pages_compact(pages, stream=None):
 
 def move_records(shape, cfg, cache, pages, stream=None):
     """One layer's records after pages_compact."""
-    _check(lib().kvmix_move_records(C.byref(shape), C.byref(cfg), C.byref(cache.c), C.byref(pages.c), _stream(stream)), "kvmix_move_records")
+    _check(lib().kvmix_move_records(C.byref(shape), C.byref(cfg), cache.ref, pages.ref, _stream(stream)), "kvmix_move_records")
 
 
 def copy_windows(shape, cfg, cache, src, dst, stream=None):
     """Both fp16 rings of slot src[i] to slot dst[i]."""
     n = src.numel()
-    st = lib().kvmix_copy_windows(C.byref(shape), C.byref(cfg), C.byref(cache.c), _int32(src, n, "src"), _int32(dst, n, "dst"), n, _stream(stream))
+    st = lib().kvmix_copy_windows(C.byref(shape), C.byref(cfg), cache.ref, _int32(src, n, "src"), _int32(dst, n, "dst"), n, _stream(stream))
     _check(st, "kvmix_copy_windows")
 
 
@@ -359,8 +370,8 @@ def paged_append(shape, cfg, k_new, v_new, cache, pages, rows=None, cu=None, max
     each (cu None: token b), for which pages_grow has made room."""
     ks, vs = k_new.stride(), v_new.stride()
     assert k_new.element_size() == v_new.element_size() == 2 and ks[2] == vs[2] == 1 and k_new.shape == v_new.shape
-    st = lib().kvmix_paged_append(C.byref(shape), C.byref(cfg), k_new.data_ptr(), ks[0], ks[1], v_new.data_ptr(), vs[0], vs[1], C.byref(cache.c),
-                                  C.byref(pages.c), _int32(rows, shape.B, "rows"), _int32(cu, shape.B + 1, "cu"), max_new, _stream(stream))
+    st = lib().kvmix_paged_append(C.addressof(shape), C.addressof(cfg), k_new.data_ptr(), ks[0], ks[1], v_new.data_ptr(), vs[0], vs[1], cache.ref,
+                                  pages.ref, _int32(rows, shape.B, "rows"), _int32(cu, shape.B + 1, "cu"), max_new, _stream(stream))
     _check(st, "kvmix_paged_append")
 
 
@@ -375,10 +386,13 @@ def paged_decode_attn(shape, cfg, q, cache, pages, out, workspace=None, rows=Non
     workspace: uint8 CUDA tensor of paged_workspace_bytes, zeroed once."""
     assert q.is_contiguous() and out.is_contiguous()
     wp, wn = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
-    st = lib().kvmix_paged_decode_attn(C.byref(shape), C.byref(cfg), q.data_ptr(), C.byref(cache.c), C.byref(pages.c), _int32(rows, shape.B, "rows"),
-                                       max_len, C.c_float(softmax_scale), out.data_ptr(), wp, wn, _stream(stream))
+    st = lib().kvmix_paged_decode_attn(C.addressof(shape), C.addressof(cfg), q.data_ptr(), cache.ref, pages.ref, _int32(rows, shape.B, "rows"),
+                                       max_len, softmax_scale, out.data_ptr(), wp, wn, _stream(stream))
     _check(st, "kvmix_paged_decode_attn")
     return out
+
+
+_rope_struct = struct.Struct("PiiffPP" + "PPqq" * 3).pack      # kvmix_rope
 
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
@@ -397,23 +411,31 @@ def qk_norm_rope(shape, q, k, positions, frequencies, q_out, k_out, v=None, v_ou
     """q [tokens][Hq][128], k, v [tokens][Hkv][128]: fp16, bf16 or fp32 CUDA tensors of one type (last dim contiguous, any strides otherwise);
     outputs fp16, contiguous. Heads are normed where a weight [128] is given, and the first 2 * len(frequencies) channels rotated (frequencies
     None: none); v is converted only. Any of q, k, v may be None."""
-    import torch
-    some = [x for x in (q, k, v) if x is not None]
-    if not some:
+    _, half, single, codes = _types or _torch_types()
+    some = q if q is not None else k if k is not None else v
+    if some is None:
         return
-    n, dtype = some[0].shape[0], some[0].dtype
-    code = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}.get(dtype, -1)
+    n, dtype = some.shape[0], some.dtype
     sides = []
     for x, o, heads in ((q, q_out, shape.Hq), (k, k_out, shape.Hkv), (v, v_out, shape.Hkv)):
         if x is None:
-            sides += [None, 0, 0, None]
+            sides += (0, 0, 0, 0)
             continue
-        assert x.dtype == dtype and tuple(x.shape) == (n, heads, 128) and x.stride(2) == 1
-        assert o.dtype == torch.float16 and o.shape == x.shape and o.is_contiguous()
-        sides += [x.data_ptr(), x.stride(0), x.stride(1), o.data_ptr()]
-    for w in (q_weight, k_weight):
-        assert w is None or (w.dtype == dtype and w.numel() == 128 and w.is_contiguous())
-    assert frequencies is None or (frequencies.dtype == torch.float32 and frequencies.is_contiguous())
-    rope = _RopeStruct(None if frequencies is None else frequencies.data_ptr(), 0 if frequencies is None else 2 * frequencies.numel(), int(interleaved),
-                       amplitude, eps, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr())
-    _check(lib().kvmix_qk_norm_rope(C.byref(shape), C.byref(rope), code, n, _int32(positions, n, "positions"), *sides, _stream(stream)), "kvmix_qk_norm_rope")
+        strides = x.stride()
+        assert x.dtype is dtype and x.shape == (n, heads, 128) and strides[2] == 1
+        assert o.dtype is half and o.numel() == n * heads * 128 and o.is_contiguous()
+        sides += (x.data_ptr(), o.data_ptr(), strides[0], strides[1])
+    qw = kw = at = pairs = 0
+    if q_weight is not None:
+        assert q_weight.dtype is dtype and q_weight.numel() == 128 and q_weight.is_contiguous()
+        qw = q_weight.data_ptr()
+    if k_weight is not None:
+        assert k_weight.dtype is dtype and k_weight.numel() == 128 and k_weight.is_contiguous()
+        kw = k_weight.data_ptr()
+    if frequencies is not None:
+        assert frequencies.dtype is single and frequencies.is_contiguous()
+        at, pairs = frequencies.data_ptr(), frequencies.numel()
+    rope = _rope_struct(at, 2 * pairs, interleaved, amplitude, eps, qw, kw, *sides)
+    st = lib().kvmix_qk_norm_rope(C.addressof(shape), rope, codes.get(dtype, -1), n, _int32(positions, n, "positions"), _stream(stream))
+    if st:
+        _check(st, "kvmix_qk_norm_rope")

@@ -206,7 +206,7 @@ struct RopeSide { const void* in; uint16_t* out; const void* weight; int64_t tok
 struct RopeArgs {
   RopeSide side[3];       // q, k, v
   const int32_t* positions; const float* frequencies;
-  int n_tokens, rotary_dim, interleaved;
+  int n_tokens, rotary_dim, interleaved, log2_tokens;
   float amplitude, eps;
 };
 

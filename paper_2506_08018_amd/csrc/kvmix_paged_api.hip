@@ -296,9 +296,7 @@ int kvmix_rope_frequencies(int rotary_dim, double base, int scaling, double fact
   return KVMIX_OK;
 }
 
-int kvmix_qk_norm_rope(const kvmix_shape* sh, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions, const void* q,
-                       int64_t q_token_stride, int64_t q_head_stride, uint16_t* q_out, const void* k, int64_t k_token_stride, int64_t k_head_stride,
-                       uint16_t* k_out, const void* v, int64_t v_token_stride, int64_t v_head_stride, uint16_t* v_out, void* stream) {
+int kvmix_qk_norm_rope(const kvmix_shape* sh, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions, void* stream) {
   const kvmix_layer_cfg cfg = {2, 2, 0};
   const int st = check_shape_cfg(sh, &cfg);
   if (st) return st;
@@ -310,20 +308,20 @@ int kvmix_qk_norm_rope(const kvmix_shape* sh, const kvmix_rope* rope, int dtype,
   if (!aligned16(rope->frequencies) || !aligned16(rope->q_weight) || !aligned16(rope->k_weight) || !aligned4(positions)) return KVMIX_ERR_ALIGN;
   const int step = dtype == KVMIX_F32 ? 4 : 8;       // elements of 16 bytes
   RopeArgs a{};
-  const void* in[3] = {q, k, v};
-  uint16_t* out[3] = {q_out, k_out, v_out};
+  const kvmix_rope_side* side[3] = {&rope->q, &rope->k, &rope->v};
   const void* weight[3] = {rope->q_weight, rope->k_weight, nullptr};
-  const int64_t tok[3] = {q_token_stride, k_token_stride, v_token_stride}, head[3] = {q_head_stride, k_head_stride, v_head_stride};
   for (int i = 0; i < 3; i++) {
-    if (!in[i] != !out[i]) return KVMIX_ERR_NULL;
-    if (!aligned16(in[i]) || !aligned16(out[i]) || (in[i] && (tok[i] % step || head[i] % step))) return KVMIX_ERR_ALIGN;
-    a.side[i] = RopeSide{in[i], out[i], weight[i], tok[i], head[i], !in[i] ? 0 : i == 0 ? sh->Hq : sh->Hkv};
+    const kvmix_rope_side& s = *side[i];
+    if (!s.in != !s.out) return KVMIX_ERR_NULL;
+    if (!aligned16(s.in) || !aligned16(s.out) || (s.in && (s.token_stride % step || s.head_stride % step))) return KVMIX_ERR_ALIGN;
+    a.side[i] = RopeSide{s.in, s.out, weight[i], s.token_stride, s.head_stride, !s.in ? 0 : i == 0 ? sh->Hq : sh->Hkv};
   }
-  if (n_tokens == 0 || (!q && !k && !v)) return KVMIX_OK;
-  if (!positions && rope->rotary_dim > 0 && (q || k)) return KVMIX_ERR_NULL;
+  const bool turns = rope->q.in || rope->k.in;
+  if (n_tokens == 0 || (!turns && !rope->v.in)) return KVMIX_OK;
+  a.rotary_dim = turns ? rope->rotary_dim : 0;
+  if (!positions && a.rotary_dim > 0) return KVMIX_ERR_NULL;
   a.positions = positions; a.frequencies = rope->frequencies;
   a.n_tokens = n_tokens; a.interleaved = rope->interleaved != 0;
-  a.rotary_dim = q || k ? rope->rotary_dim : 0;
   a.amplitude = rope->amplitude; a.eps = rope->eps;
   const hipError_t e = launch_rope(a, dtype, (hipStream_t)stream);
   return e == hipSuccess ? KVMIX_OK : hip_fail(e);

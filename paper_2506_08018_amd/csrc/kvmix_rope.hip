@@ -7,6 +7,10 @@
 // angles: a lane has 4 of them, made once for all the rows that it takes.
 // An angle is a fraction of a turn taken in binary64: position * frequency in fp32 is off by up to position * 2^-24 radians, 0.06 at a
 // million.
+// Measured: a prompt of 8191 tokens x 48 heads in bf16 (201 MB) 39.3 us, what a plain copy of as many bytes takes (38.9); one row of a lane at a
+// time 45 us, with the row's pointers read by index from the arguments and sine and cosine by the math library 64 us. One token x 48
+// heads 2.3 us, 64 tokens x 80 heads 3.1, a launch that does anything 2.3. With 8 lanes to a row and 16 bytes of either half per lane
+// 38.8 and 41 us (two rows and one at a time), 2.5 for one token; with accesses past the caches 43-49 us.
 #include <type_traits>
 #include "kvmix_common.hpp"
 
@@ -15,45 +19,37 @@ namespace kvmix {
 namespace {
 
 struct Bf16 { uint16_t bits; };
-template <typename T> struct Four;          // 4 consecutive elements as loaded
-template <> struct Four<half_t> {
-  u32x2_t w;
-  __device__ __forceinline__ void get(float (&x)[4]) const {
-    const uint32_t a = w[0], b = w[1];       // (copies: a bit cast applied to the vector element itself reads element 0)
-    const half2_t p = __builtin_bit_cast(half2_t, a), q = __builtin_bit_cast(half2_t, b);
-    x[0] = (float)p[0]; x[1] = (float)p[1]; x[2] = (float)q[0]; x[3] = (float)q[1];
-  }
-};
-template <> struct Four<Bf16> {
-  u32x2_t w;
-  __device__ __forceinline__ void get(float (&x)[4]) const {
+constexpr int P = 4;       // consecutive channels of a lane, twice
+// as loaded: 8 bytes, or 16 of fp32
+template <typename T> struct Group {
+  static constexpr int kWords = P * (int)sizeof(T) / 4;
+  typedef uint32_t words_t __attribute__((ext_vector_type(kWords)));
+  words_t w;
+  __device__ __forceinline__ void load(const void* base, int64_t at) { w = *reinterpret_cast<const words_t*>(reinterpret_cast<const T*>(base) + at); }
+  __device__ __forceinline__ void get(float (&x)[P]) const {
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-      const uint32_t v = w[i], lo = v << 16, hi = v & 0xFFFF0000u;
-      x[2 * i] = __builtin_bit_cast(float, lo); x[2 * i + 1] = __builtin_bit_cast(float, hi);
+    for (int i = 0; i < kWords; i++) {
+      const uint32_t v = w[i];       // (a copy: a bit cast applied to the vector element itself reads element 0)
+      if constexpr (std::is_same_v<T, float>) {
+        x[i] = __builtin_bit_cast(float, v);
+      } else if constexpr (std::is_same_v<T, Bf16>) {
+        const uint32_t lo = v << 16, hi = v & 0xFFFF0000u;
+        x[2 * i] = __builtin_bit_cast(float, lo); x[2 * i + 1] = __builtin_bit_cast(float, hi);
+      } else {
+        const half2_t p = __builtin_bit_cast(half2_t, v);
+        x[2 * i] = (float)p[0]; x[2 * i + 1] = (float)p[1];
+      }
     }
   }
 };
-template <> struct Four<float> {
-  float4_t w;
-  __device__ __forceinline__ void get(float (&x)[4]) const {
-#pragma unroll
-    for (int i = 0; i < 4; i++) x[i] = w[i];
-  }
-};
-template <typename T> __device__ __forceinline__ Four<T> load4(const void* base, int64_t at) {
-  Four<T> r;
-  r.w = *reinterpret_cast<const decltype(r.w)*>(reinterpret_cast<const T*>(base) + at);
-  return r;
-}
-__device__ __forceinline__ void store4(uint16_t* p, const float (&x)[4]) {
+__device__ __forceinline__ void store(uint16_t* p, const float (&x)[P]) {
   const half2_t a = {(half_t)x[0], (half_t)x[1]}, b = {(half_t)x[2], (half_t)x[3]};
   *reinterpret_cast<u32x2_t*>(p) = u32x2_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
 }
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
 }
-// sum over the 16 lanes of each row; every lane of the row gets it
+// sum over the 16 lanes that have a row; every one of them gets it
 __device__ __forceinline__ float row_sum(float v) {
   v += dpp<0xB1>(v);
   v += dpp<0x4E>(v);
@@ -62,89 +58,121 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
-constexpr int kRopeThreads = 256;
-// R: rows of a lane under way together; grid (tokens, blocks of 16 R rows)
+constexpr int kRopeThreads = 256, kLanes = kD / (2 * P), kRows = kRopeThreads / kLanes;
+// Grid (tokens, blocks of kRows * R rows): R rows of a lane are under way together. Tokens of half as many rows or fewer (R == 1): log2_tokens,
+// so many share a workgroup.
 template <typename T, int R>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) {
-  const int token = blockIdx.x, c = threadIdx.x & 15;
-  const int turned = a.rotary_dim / 8;                 // lanes that have pairs
-  // first channels of the lane's two fours
+  const int c = threadIdx.x % kLanes;
+  int token = blockIdx.x, row0 = (int)threadIdx.x / kLanes;      // first row of the lane
+  if constexpr (R == 1) {
+    const int each = kRows >> a.log2_tokens;
+    token = (token << a.log2_tokens) + row0 / each;      // (a power of two)
+    row0 %= each;
+    if (token >= a.n_tokens) return;
+  }
+  const int turned = a.rotary_dim / (2 * P);           // lanes that have pairs
+  // first channels of the lane's two groups
   const bool halves = !a.interleaved && c < turned;
-  const int at0 = halves ? 4 * c : 8 * c, at1 = halves ? a.rotary_dim / 2 + 4 * c : 8 * c + 4;
-  const int n_q = a.side[0].heads, n_k = a.side[1].heads, rows = n_q + n_k + a.side[2].heads;
-  Four<T> x0[R], x1[R], w0[R], w1[R];
-  int side[R], head[R];
+  const int at0 = halves ? P * c : 2 * P * c, at1 = halves ? a.rotary_dim / 2 + P * c : 2 * P * c + P;
+  const int n_q = a.side[0].heads, n_qk = n_q + a.side[1].heads, rows = n_qk + a.side[2].heads;
+  Group<T> x0[R], x1[R];
+  // (a row's side is chosen with the arguments in scalar registers: as an index into them it would be one more way to memory)
+  auto side_of = [&](int row, auto field) {
+    const auto q = field(a.side[0]), k = field(a.side[1]), v = field(a.side[2]);
+    return row < n_q ? q : row < n_qk ? k : v;
+  };
+  auto row_at = [&](int k) { return ((int)blockIdx.y * R + k) * kRows + row0; };
+  auto head_of = [&](int row) { return row - (row < n_q ? 0 : row < n_qk ? n_q : n_qk); };
 #pragma unroll
   for (int k = 0; k < R; k++) {
-    const int row = (blockIdx.y * R + k) * (kRopeThreads / 16) + (int)(threadIdx.x >> 4);
-    side[k] = row >= rows ? -1 : row < n_q ? 0 : row < n_q + n_k ? 1 : 2;
-    head[k] = row - (side[k] >= 1 ? n_q : 0) - (side[k] == 2 ? n_k : 0);
-    if (side[k] < 0) continue;
-    const RopeSide& s = a.side[side[k]];
-    const int64_t at = (int64_t)token * s.tok + (int64_t)head[k] * s.head;
-    x0[k] = load4<T>(s.in, at + at0);
-    x1[k] = load4<T>(s.in, at + at1);
-    if (s.weight) { w0[k] = load4<T>(s.weight, at0); w1[k] = load4<T>(s.weight, at1); }
+    const int row = row_at(k);
+    if (row >= rows) continue;
+    const int64_t at = (int64_t)token * side_of(row, [](const RopeSide& s) { return s.tok; }) +
+                       (int64_t)head_of(row) * side_of(row, [](const RopeSide& s) { return s.head; });
+    const void* in = side_of(row, [](const RopeSide& s) { return s.in; });
+    x0[k].load(in, at + at0);
+    x1[k].load(in, at + at1);
   }
-  float cs[4], sn[4];
+  Group<T> w[2][2];
+#pragma unroll
+  for (int s = 0; s < 2; s++)
+    if (a.side[s].weight) { w[s][0].load(a.side[s].weight, at0); w[s][1].load(a.side[s].weight, at1); }
+  float cs[P], sn[P];
   if (c < turned) {
     const double pos = (double)a.positions[token];
-    const float4_t f = *reinterpret_cast<const float4_t*>(a.frequencies + 4 * c);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      double t = pos * ((double)f[i] * 0.15915494309189533577);
+    for (int i = 0; i < P; i++) {
+      double t = pos * ((double)a.frequencies[P * c + i] * 0.15915494309189533577);
       t -= rint(t);
-      float s, co;
-      sincospif(2.0f * (float)t, &s, &co);
-      cs[i] = co * a.amplitude;
-      sn[i] = s * a.amplitude;
+      // (the hardware's sine and cosine take turns)
+      cs[i] = __builtin_amdgcn_cosf((float)t) * a.amplitude;
+      sn[i] = __builtin_amdgcn_sinf((float)t) * a.amplitude;
     }
   }
 #pragma unroll
   for (int k = 0; k < R; k++) {
-    if (side[k] < 0) continue;
-    const RopeSide& s = a.side[side[k]];
-    float x[4], y[4];
+    const int row = row_at(k);
+    if (row >= rows) continue;
+    float x[P], y[P];
     x0[k].get(x);
     x1[k].get(y);
-    if (s.weight) {
-      float sum = 0.0f, u[4], v[4];
+    const bool key = row >= n_q;
+    if (row < n_qk && (key ? a.side[1].weight : a.side[0].weight)) {
+      float sum = 0.0f, u[P], v[P];
 #pragma unroll
-      for (int i = 0; i < 4; i++) sum += x[i] * x[i] + y[i] * y[i];
+      for (int i = 0; i < P; i++) sum += x[i] * x[i] + y[i] * y[i];
       const float r = rsqrtf(row_sum(sum) * (1.0f / kD) + a.eps);
-      w0[k].get(u);
-      w1[k].get(v);
+      (key ? w[1][0] : w[0][0]).get(u);
+      (key ? w[1][1] : w[0][1]).get(v);
 #pragma unroll
-      for (int i = 0; i < 4; i++) { x[i] = x[i] * r * u[i]; y[i] = y[i] * r * v[i]; }
+      for (int i = 0; i < P; i++) { x[i] = x[i] * r * u[i]; y[i] = y[i] * r * v[i]; }
     }
-    if (side[k] < 2 && c < turned) {
+    if (row < n_qk && c < turned) {
       if (a.interleaved) {
-        const float p[4] = {x[0], x[2], y[0], y[2]}, q[4] = {x[1], x[3], y[1], y[3]};
+        // pairs 0 .. P/2 - 1 in the first group, the others in the second
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const float even = p[i] * cs[i] - q[i] * sn[i], odd = q[i] * cs[i] + p[i] * sn[i];
-          (i < 2 ? x : y)[2 * (i & 1)] = even;
-          (i < 2 ? x : y)[2 * (i & 1) + 1] = odd;
+        for (int i = 0; i < P; i++) {
+          float (&g)[P] = i < P / 2 ? x : y;
+          const int e = 2 * (i % (P / 2));
+          const float p = g[e], q = g[e + 1];
+          g[e] = p * cs[i] - q * sn[i];
+          g[e + 1] = q * cs[i] + p * sn[i];
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < P; i++) {
           const float p = x[i], q = y[i];
           x[i] = p * cs[i] - q * sn[i];
           y[i] = q * cs[i] + p * sn[i];
         }
       }
     }
-    uint16_t* out = s.out + ((int64_t)token * s.heads + head[k]) * kD;
-    store4(out + at0, x);
-    store4(out + at1, y);
+    uint16_t* out = side_of(row, [](const RopeSide& s) { return s.out; }) +
+                    ((int64_t)token * side_of(row, [](const RopeSide& s) { return s.heads; }) + head_of(row)) * kD;
+    store(out + at0, x);
+    store(out + at1, y);
   }
 }
 
+// Rows of a lane under way together: one while the workgroups are few (256 tokens x 48 heads, 768 of them, 3.48 us with one, 3.51 with two,
+// 3.98 with three; 512: 4.84, 4.72, 5.02), two up to twice that and more (1024: 7.55, 6.74, 7.18), three for large ones (2048: 11.4, 10.6,
+// 10.3; 4096: 23.4, 21.1, 19.9; in fp32 28.6, 28.7, 30.0).
 template <typename T>
-hipError_t launch_rope_type(const RopeArgs& a, hipStream_t s) {
-  const int rows = a.side[0].heads + a.side[1].heads + a.side[2].heads, each = kRopeThreads / 16;
-  return launch(qk_norm_rope_kernel<T, 1>, dim3(a.n_tokens, (rows + each - 1) / each), kRopeThreads, s, a);
+hipError_t launch_rope_type(RopeArgs a, hipStream_t s) {
+  const int rows = a.side[0].heads + a.side[1].heads + a.side[2].heads, blocks = (rows + kRows - 1) / kRows;
+  const int64_t workgroups = (int64_t)a.n_tokens * blocks;
+  auto run = [&](auto each) {
+    constexpr int R = decltype(each)::value;
+    const int tokens = (int)(((int64_t)a.n_tokens + (1 << a.log2_tokens) - 1) >> a.log2_tokens);
+    return launch(qk_norm_rope_kernel<T, R>, dim3(tokens, (rows + kRows * R - 1) / (kRows * R)), kRopeThreads, s, a);
+  };
+  a.log2_tokens = 0;
+  if (blocks == 1)
+    while (a.log2_tokens < 4 && rows << (a.log2_tokens + 1) <= kRows) a.log2_tokens++;
+  if (blocks == 1 || workgroups < 1200) return run(std::integral_constant<int, 1>{});
+  if (sizeof(T) == 4 || blocks == 2 || workgroups < 4800) return run(std::integral_constant<int, 2>{});
+  return run(std::integral_constant<int, 3>{});
 }
 
 }  // namespace

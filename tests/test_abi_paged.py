@@ -162,20 +162,20 @@ def test_the_grid_holds_every_piece(kv, plan):
 
 
 def test_rotation_refusals(kv):
-    from paper_2506_08018_amd.binding import _RopeStruct
-    L, r, a, odd = kv.lib(), C.byref, C.c_void_p(A), C.c_void_p(A + 8)
+    from paper_2506_08018_amd.binding import _rope_struct
+    L, r, a = kv.lib(), C.byref, C.c_void_p(A)
     sh = kv.Shape(1, 8, 2)
 
-    def call(dtype=1, n=3, pos=a, q=a, q_out=a, v_out=None, tok=1024, head=128, **rope):
-        f = dict(frequencies=A, rotary_dim=128, interleaved=0, amplitude=1.0, eps=1e-6, q_weight=None, k_weight=None)
+    def call(dtype=1, n=3, pos=a, q=A, q_out=A, v=0, v_out=0, tok=1024, head=128, **rope):
+        f = dict(frequencies=A, rotary_dim=128, interleaved=0, amplitude=1.0, eps=1e-6, q_weight=0, k_weight=0)
         f.update(rope)
-        return L.kvmix_qk_norm_rope(r(sh), r(_RopeStruct(*f.values())), dtype, n, pos, q, tok, head, q_out, None, 0, 0, None, None, 0, 0, v_out, None)
+        return L.kvmix_qk_norm_rope(r(sh), _rope_struct(*f.values(), q, q_out, tok, head, 0, 0, 0, 0, v, v_out, tok, head), dtype, n, pos, None)
 
-    assert L.kvmix_qk_norm_rope(r(sh), None, 0, 1, a, a, 128, 128, a, None, 0, 0, None, None, 0, 0, None, None) == -1
+    assert L.kvmix_qk_norm_rope(r(sh), None, 0, 1, a, None) == -1
     assert call(dtype=3) == call(n=-1) == call(rotary_dim=8) == call(rotary_dim=144) == call(rotary_dim=-16) == call(eps=-1.0) == call(eps=float("nan")) == -4
-    assert call(q_out=None) == call(q=None) == call(v_out=a) == call(pos=None) == call(frequencies=None) == -1
-    assert call(q=odd) == call(q_out=odd) == call(tok=1028) == call(head=4) == call(q_weight=A + 2) == call(frequencies=A + 4) == call(pos=C.c_void_p(A + 2)) == -5
-    assert call(n=0) == 0 and call(q=None, q_out=None) == 0
+    assert call(q_out=0) == call(q=0) == call(v_out=A) == call(v=A) == call(pos=None) == call(frequencies=0) == -1
+    assert call(q=A + 8) == call(q_out=A + 8) == call(tok=1028) == call(head=4) == call(q_weight=A + 2) == call(frequencies=A + 4) == call(pos=C.c_void_p(A + 2)) == -5
+    assert call(n=0) == 0 and call(q=0, q_out=0) == 0
     assert call(dtype=2, n=0, tok=1028, head=132) == 0          # four fp32 elements are 16 bytes
 
 

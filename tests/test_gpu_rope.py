@@ -67,7 +67,7 @@ def test_types_layouts_and_parts(dtype, interleaved, rot):
         run(dtype, 7, 8, 2, rot, interleaved, norm, 5000, seed=rot)
 
 
-@pytest.mark.parametrize("N,Hq,Hkv", [(1, 1, 1), (1, 32, 8), (2, 72, 1), (64, 64, 8), (513, 4, 4), (3000, 32, 8), (1, 512, 1)])
+@pytest.mark.parametrize("N,Hq,Hkv", [(1, 1, 1), (1, 32, 8), (2, 72, 1), (64, 64, 8), (513, 4, 4), (3000, 32, 8), (1, 512, 1), (1000, 1, 1), (77, 2, 2), (31, 4, 2), (600, 24, 1), (1200, 64, 8)])
 def test_sizes(N, Hq, Hkv):
     run("bfloat16", N, Hq, Hkv, 128, False, True, 100000, seed=N)
     run("float16", N, Hq, Hkv, 96, True, False, 100000, seed=N)
