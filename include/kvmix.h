@@ -358,11 +358,11 @@ int kvmix_copy_windows(const kvmix_shape* shape, const kvmix_layer_cfg* cfg, con
 /* kvmix_append_tokens for a ragged batch, after kvmix_pages_grow: the tokens [cu[b], cu[b + 1]) of k_new, v_new (element (i, j, d) of
  * each at i*token_stride + j*head_stride + d; strides of their own, in elements, multiples of 8, not negative; 16-byte aligned) are the newest of
  * slot rows[b], b < shape->B. Tiles that fall due are quantized into their pages exactly as in kvmix_quantize_pack, from the ring or
- * straight from the input; what stays goes into the ring; one launch. max_new: no row brings more tokens (the grid's size). A
- * row whose token count is not what grown[s] says, or exceeds max_new, is left alone. */
+ * straight from the input; what stays goes into the ring; one launch. n_tokens: tokens of the inputs. max_new: no row brings more. A
+ * row whose token count is not what grown[s] says, exceeds max_new or goes past n_tokens is left alone. */
 int kvmix_paged_append(const kvmix_shape* shape, const kvmix_layer_cfg* cfg,
                        const uint16_t* k_new, int64_t k_token_stride, int64_t k_head_stride,
-                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride,
+                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride, int n_tokens,
                        const kvmix_paged_cache* cache, const kvmix_pages* pages,
                        const int32_t* rows, const int32_t* cu, int max_new, void* stream);
 

@@ -75,7 +75,7 @@ def lib():
         L.kvmix_flush.argtypes = [P, P, P, I, I, P]
         for name, args in (("kvmix_pages_grow", [P, P, P, I, P]), ("kvmix_pages_free", [P, P, I, P]), ("kvmix_pages_fork", [P, P, P, I, P]),
                            ("kvmix_pages_compact", [P, P]), ("kvmix_move_records", [P] * 5), ("kvmix_copy_windows", [P] * 5 + [I, P]),
-                           ("kvmix_paged_append", [P, P] + [P, I64, I64] * 2 + [P] * 4 + [I, P]), ("kvmix_paged_workspace_bytes", [P, I, P]),
+                           ("kvmix_paged_append", [P, P] + [P, I64, I64] * 2 + [I] + [P] * 4 + [I, P]), ("kvmix_paged_workspace_bytes", [P, I, P]),
                            ("kvmix_paged_decode_attn", [P] * 6 + [I, C.c_float, P, P, SZ, P]),
                            ("kvmix_rope_frequencies", [I, C.c_double, I, C.c_double, I, C.c_double, C.c_double, P, P]),
                            ("kvmix_qk_norm_rope", [P, P, I, I, P, P])):
@@ -368,9 +368,9 @@ def copy_windows(shape, cfg, cache, src, dst, stream=None):
 def paged_append(shape, cfg, k_new, v_new, cache, pages, rows=None, cu=None, max_new=1, stream=None):
     """k_new, v_new: fp16 CUDA tensors [tokens][Hkv][128] (last dim contiguous, any strides otherwise), the tokens [cu[b], cu[b + 1]) of batch row b, at most max_new
     each (cu None: token b), for which pages_grow has made room."""
-    ks, vs = k_new.stride(), v_new.stride()
-    assert k_new.element_size() == v_new.element_size() == 2 and ks[2] == vs[2] == 1 and k_new.shape == v_new.shape
-    st = lib().kvmix_paged_append(C.addressof(shape), C.addressof(cfg), k_new.data_ptr(), ks[0], ks[1], v_new.data_ptr(), vs[0], vs[1], cache.ref,
+    half, ks, vs, size = (_types or _torch_types())[1], k_new.stride(), v_new.stride(), k_new.shape
+    assert k_new.dtype is half and v_new.dtype is half and ks[2] == vs[2] == 1 and v_new.shape == size and size[1:] == (shape.Hkv, 128)
+    st = lib().kvmix_paged_append(C.addressof(shape), C.addressof(cfg), k_new.data_ptr(), ks[0], ks[1], v_new.data_ptr(), vs[0], vs[1], size[0], cache.ref,
                                   pages.ref, _int32(rows, shape.B, "rows"), _int32(cu, shape.B + 1, "cu"), max_new, _stream(stream))
     _check(st, "kvmix_paged_append")
 

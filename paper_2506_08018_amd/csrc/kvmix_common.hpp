@@ -197,6 +197,8 @@ struct PagedAppendArgs {
   int64_t v_tok, v_head;
   const int32_t* rows; const int32_t* cu; const int32_t* lens; const int32_t* grown; const int32_t* table;
   int32_t* status;
+  int B, n_tokens, more;  // batch rows; tokens of the inputs; tiles of a row beyond a 32nd of its tokens
+  uint32_t head_magic;    // floor(2^32 / Hkv) + 1 (0 for one kv head)
   int n_slots, n_pages, max_tiles, window, max_new;
   int ring_tiles;
   uint32_t ring_magic;
@@ -250,7 +252,7 @@ template <> hipError_t launch_decode_attn<12, true>(const AttnArgs& a, int k_bit
 
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s);
-hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, int B, hipStream_t s);
+hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t s);
 hipError_t launch_pages_grow(const kvmix_pages& p, const int32_t* rows, const int32_t* cu, int n, hipStream_t s);
 hipError_t launch_pages_free(const kvmix_pages& p, const int32_t* rows, int n, hipStream_t s);

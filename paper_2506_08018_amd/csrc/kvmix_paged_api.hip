@@ -12,8 +12,8 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 int check_pages(const kvmix_pages* p) {
   if (!p || !p->table || !p->lens || !p->grown || !p->refs || !p->used || !p->status) return KVMIX_ERR_NULL;
   if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->grown) || !aligned4(p->refs) || !aligned4(p->used) || !aligned4(p->status)) return KVMIX_ERR_ALIGN;
-  // (page counts to 4 M: the grow kernel keeps one of 1024 counters for every 4096)
-  if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages > (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 23)) return KVMIX_ERR_BAD_SHAPE;
+  // (fewer than 4 M pages: sums over the workgroup of the grow kernel fit 32 bits)
+  if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages >= (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 23)) return KVMIX_ERR_BAD_SHAPE;
   if (p->window < 0 || p->window % kTile) return KVMIX_ERR_BAD_SHAPE;
   return KVMIX_OK;
 }
@@ -170,7 +170,7 @@ int kvmix_copy_windows(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const 
 }
 
 int kvmix_paged_append(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const uint16_t* k_new, int64_t k_token_stride, int64_t k_head_stride,
-                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride, const kvmix_paged_cache* c, const kvmix_pages* p, const int32_t* rows, const int32_t* cu, int max_new,
+                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride, int n_tokens, const kvmix_paged_cache* c, const kvmix_pages* p, const int32_t* rows, const int32_t* cu, int max_new,
                        void* stream) {
   int st = check_paged_cfg(sh, cfg);
   if (st) return st;
@@ -180,9 +180,9 @@ int kvmix_paged_append(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const 
   if (st) return st;
   st = check_together(sh, cfg, c, p);
   if (st) return st;
-  if (max_new < 0 || (!cu && max_new > 1)) return KVMIX_ERR_BAD_SHAPE;
+  if (max_new < 0 || n_tokens < 0 || (!cu && (max_new > 1 || n_tokens < sh->B))) return KVMIX_ERR_BAD_SHAPE;
   if (!aligned4(rows) || !aligned4(cu)) return KVMIX_ERR_ALIGN;
-  if (max_new == 0) return KVMIX_OK;
+  if (max_new == 0 || n_tokens == 0) return KVMIX_OK;
   if (!k_new || !v_new) return KVMIX_ERR_NULL;
   if (!aligned16(k_new) || !aligned16(v_new)) return KVMIX_ERR_ALIGN;
   for (const int64_t x : {k_token_stride, k_head_stride, v_token_stride, v_head_stride})
@@ -198,7 +198,13 @@ int kvmix_paged_append(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const 
   a.n_slots = p->n_slots; a.n_pages = p->n_pages; a.max_tiles = p->max_tiles; a.window = p->window; a.max_new = max_new;
   a.ring_tiles = c->W_cap / kTile;
   a.ring_magic = ring_magic(a.ring_tiles);
-  const hipError_t e = launch_paged_append(a, cfg->k_bits, cfg->v_bits, sh->B, (hipStream_t)stream);
+  a.B = sh->B; a.n_tokens = n_tokens;
+  // rows that stay lie in two ring tiles if they are no more than a tile, and in all of them at worst; one tile for what is due beyond a 32nd
+  a.more = 1 + (max_new <= kTile && a.ring_tiles > 2 ? 2 : a.ring_tiles);
+  a.head_magic = ring_magic(sh->Hkv);
+  const long long tiles = (long long)n_tokens / kTile + (long long)sh->B * a.more + 1;
+  if (tiles * sh->Hkv * sh->Hkv >= (1LL << 32) || tiles > 0x7fffffffLL) return KVMIX_ERR_BAD_SHAPE;
+  const hipError_t e = launch_paged_append(a, cfg->k_bits, cfg->v_bits, (hipStream_t)stream);
   return e == hipSuccess ? KVMIX_OK : hip_fail(e);
 }
 

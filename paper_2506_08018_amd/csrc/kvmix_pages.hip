@@ -11,32 +11,37 @@ namespace kvmix {
 
 namespace {
 
-constexpr int kGrowThreads = 1024;
+constexpr int kGrowThreads = 1024, kGrowWaves = kGrowThreads / kWave;
 constexpr int kMaxRows = 4096;                        // of one call of grow or fork
-constexpr int kRowsEach = kMaxRows / kGrowThreads;
-constexpr int kChunk = 4096;                          // page ids that are looked at together: four bits to a thread
-constexpr int kMaxChunks = 1024;                      // 4 M pages
+constexpr int kMostPages = (1 << 22) - 1;
 
-// sum over the workgroup's threads before this one; total: over all of them (all threads call it)
-template <typename T>
-__device__ T scan_before(T v, T* s_wave, T& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  T x = v;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const T y = __shfl_up(x, d);
-    x += lane >= d ? y : 0;
-  }
-  __syncthreads();                                    // (s_wave may still be read)
+template <int CTRL, int ROW_MASK = 0xf>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xf, false); }
+// sum over the wave's lanes up to this one
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += dpp<0x111>(v);          // row_shr
+  v += dpp<0x112>(v);
+  v += dpp<0x114>(v);
+  v += dpp<0x118>(v);
+  v += dpp<0x142, 0xA>(v);     // row_bcast:15, :31
+  v += dpp<0x143, 0xC>(v);
+  return v;
+}
+// Sums over the workgroup's threads before this one, of two numbers at once; totals over all of them. s_wave is the call's own (no barrier
+// in front of its first use, one behind).
+struct Two { uint32_t a, b; };
+__device__ __forceinline__ Two scan_before(Two v, Two (&s_wave)[kGrowWaves], Two& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Two x = {wave_scan(v.a), wave_scan(v.b)};
   if (lane == kWave - 1) s_wave[wave] = x;
   __syncthreads();
-  T before = 0, all = 0;
-  for (int w = 0; w < waves; w++) {
-    before += w < wave ? s_wave[w] : 0;
-    all += s_wave[w];
-  }
-  total = all;
-  return before + x - v;
+  const Two w = s_wave[lane % kGrowWaves], upto = {wave_scan(lane < kGrowWaves ? w.a : 0), wave_scan(lane < kGrowWaves ? w.b : 0)};
+  auto at = [](uint32_t y, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)y, l); };
+  total = {at(upto.a, kGrowWaves - 1), at(upto.b, kGrowWaves - 1)};
+  const int before = __builtin_amdgcn_readfirstlane(wave) - 1;
+  Two r = {x.a - v.a, x.b - v.b};
+  if (before >= 0) { r.a += at(upto.a, before); r.b += at(upto.b, before); }
+  return r;
 }
 
 __device__ __forceinline__ uint32_t valid_bits(int word, int n_pages) {
@@ -44,100 +49,124 @@ __device__ __forceinline__ uint32_t valid_bits(int word, int n_pages) {
   return left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
 }
 
-// One workgroup: rows first (what each needs, in their order), then as many of the lowest free ids as are granted, a chunk of 4096 pages at
-// a time, chunks without a free page skipped. Ranks of free ids meet rows by binary search over the rows' first ranks.
+// One workgroup: what each row needs, in the rows' order, and how much there is, in one scan; then the lowest free ids that are granted, 32768 pages
+// at a time, a word of bits to a thread. Ranks of free ids meet rows by binary search over the rows' first ranks. A slot that is named
+// twice is looked for only if two rows meet in a table of 32768 bits. 32 rows with 1000 pages to take from 10 000: 16 us with
+// chunks of 4096 ids, cross-lane sums through LDS and a comparison of every two rows, 4.3 now.
+// EACH: rows of a thread, in a row.
+constexpr int kBits = 32768, kIds = 4096;
+template <int EACH>
 __global__ __launch_bounds__(kGrowThreads) void pages_grow_kernel(kvmix_pages p, const int32_t* rows, const int32_t* cu, int n) {
-  __shared__ int s_row[kMaxRows], s_first[kMaxRows], s_before[kMaxRows];
-  __shared__ int s_id[kChunk];
-  __shared__ int s_free[kMaxChunks];
-  __shared__ int s_wave[kGrowThreads / kWave];
-  __shared__ long long s_wave_needs[kGrowThreads / kWave];
-  __shared__ int s_granted, s_status;
-  const int tid = threadIdx.x, words = (p.n_pages + 31) / 32, chunks = (p.n_pages + kChunk - 1) / kChunk;
-  if (tid == 0) { s_granted = 0; s_status = 0; }
-  for (int c = tid; c < chunks; c += kGrowThreads) s_free[c] = 0;
-  for (int i = tid; i < kMaxRows; i += kGrowThreads) s_row[i] = i < n ? (rows ? rows[i] : i) : -1;
-  __syncthreads();
-  int free_here = 0;
-  for (int w = tid; w < words; w += kGrowThreads) {
-    const int f = __popc(~p.used[w] & valid_bits(w, p.n_pages));
-    free_here += f;
-    if (f) atomicAdd(&s_free[w / (kChunk / 32)], f);
-  }
-  int status = 0, need[kRowsEach], len[kRowsEach], fresh[kRowsEach], tiles[kRowsEach];
-  long long sum = 0;
-  bool ok[kRowsEach];
+  constexpr int kRows = EACH * kGrowThreads;
+  __shared__ int s_row[kRows], s_first[kRows], s_before[kRows];
+  __shared__ int s_id[kIds];
+  __shared__ uint32_t s_bits[kBits / 32];
+  __shared__ Two s_wave[2][kGrowWaves];
+  __shared__ int s_granted, s_status, s_twice;
+  const int tid = threadIdx.x, words = (p.n_pages + 31) / 32;
+  // (in flight together: the first words of bits, the rows, the counts)
+  const uint32_t first_bits = tid < words ? ~p.used[tid] & valid_bits(tid, p.n_pages) : 0u;
+  int row[EACH], status = 0, need[EACH], len[EACH], fresh[EACH], tiles[EACH];
+  bool ok[EACH];
 #pragma unroll
-  for (int e = 0; e < kRowsEach; e++) {
-    const int i = tid * kRowsEach + e, row = s_row[i];
-    ok[e] = false; need[e] = 0; len[e] = 0; fresh[e] = 0; tiles[e] = 0;
-    if (i < n && row >= 0) {
-      bool good = row < p.n_slots;
-      for (int j = 0; j < i && good; j++) good = s_row[j] != row;
-      if (good) {
-        len[e] = p.lens[row];
-        const int64_t add = cu ? (int64_t)cu[i + 1] - cu[i] : 1;
-        good = len[e] >= 0 && add >= 0 && add + len[e] <= 0x7fffffff;
-        fresh[e] = (int)add;
-      }
-      if (!good) status |= KVMIX_PAGES_BAD_ROW;
-      if (good) {
-        tiles[e] = packed_tiles(len[e], p.window);
-        const int after = packed_tiles(len[e] + fresh[e], p.window);
-        ok[e] = after <= p.max_tiles;
-        if (ok[e]) need[e] = after - tiles[e];
-        else { status |= KVMIX_PAGES_EXHAUSTED; p.grown[row] = 0; }
-      }
+  for (int e = 0; e < EACH; e++) {
+    const int i = tid * EACH + e;
+    row[e] = i < n ? (rows ? rows[i] : i) : -1;
+    s_row[i] = row[e];
+    ok[e] = row[e] >= 0 && row[e] < p.n_slots;
+    if (row[e] >= p.n_slots) status = KVMIX_PAGES_BAD_ROW;
+    fresh[e] = 1;
+    if (cu && i < n) {
+      const int64_t add = (int64_t)cu[i + 1] - cu[i];
+      fresh[e] = add >= 0 && add <= 0x7fffffff ? (int)add : -1;
     }
-    sum += need[e];
   }
-  int n_free;
-  long long all;
-  scan_before(free_here, s_wave, n_free);
-  long long at = scan_before(sum, s_wave_needs, all);
+  s_bits[tid] = 0;
+  if (tid == 0) { s_granted = 0; s_status = 0; s_twice = 0; }
+  __syncthreads();
 #pragma unroll
-  for (int e = 0; e < kRowsEach; e++) {
-    const int i = tid * kRowsEach + e;
-    s_first[i] = at < 0x7fffffff ? (int)at : 0x7fffffff; s_before[i] = tiles[e];
+  for (int e = 0; e < EACH; e++) {
+    len[e] = ok[e] ? p.lens[row[e]] : 0;
+    if (ok[e]) {
+      const uint32_t bit = 1u << (row[e] & 31);
+      if (atomicOr(&s_bits[row[e] / 32 % (kBits / 32)], bit) & bit) s_twice = 1;
+    }
+  }
+  uint32_t free_here = __popc(first_bits), sum = 0;
+  for (int w = tid + kGrowThreads; w < words; w += kGrowThreads) free_here += __popc(~p.used[w] & valid_bits(w, p.n_pages));
+  __syncthreads();
+  if (s_twice) {
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+      bool again = false;
+      for (int j = 0; j < tid * EACH + e; j++) again |= s_row[j] == row[e];
+      if (again && ok[e]) { ok[e] = false; status |= KVMIX_PAGES_BAD_ROW; }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < EACH; e++) {
+    need[e] = 0; tiles[e] = 0;
+    if (ok[e] && (len[e] < 0 || fresh[e] < 0 || fresh[e] > 0x7fffffff - len[e])) { ok[e] = false; status |= KVMIX_PAGES_BAD_ROW; }
+    if (ok[e]) {
+      tiles[e] = packed_tiles(len[e], p.window);
+      const int after = packed_tiles(len[e] + fresh[e], p.window);
+      if (after <= p.max_tiles) need[e] = after - tiles[e];
+      else { ok[e] = false; status |= KVMIX_PAGES_EXHAUSTED; p.grown[row[e]] = 0; }
+    }
+    sum += (uint32_t)need[e];
+  }
+  // (a thread's needs count up to kMostPages: what is more is more than there is, and 1024 of them fit 32 bits)
+  Two all;
+  const Two before = scan_before({free_here, sum < (uint32_t)kMostPages ? sum : (uint32_t)kMostPages}, s_wave[0], all);
+  const int n_free = (int)all.a;
+  int at = before.b < (1u << 24) ? (int)before.b : 1 << 24;
+#pragma unroll
+  for (int e = 0; e < EACH; e++) {
+    const int i = tid * EACH + e;
+    s_first[i] = at; s_before[i] = tiles[e];
     at += need[e];
     const bool granted = ok[e] && (need[e] == 0 || at <= n_free);
-    if (granted && need[e]) atomicMax(&s_granted, (int)at);
-    if (granted) { p.lens[s_row[i]] = len[e] + fresh[e]; p.grown[s_row[i]] = fresh[e]; }
-    else if (ok[e]) { p.grown[s_row[i]] = 0; status |= KVMIX_PAGES_EXHAUSTED; }
+    if (granted && need[e]) atomicMax(&s_granted, at);
+    if (granted) { p.lens[row[e]] = len[e] + fresh[e]; p.grown[row[e]] = fresh[e]; }
+    else if (ok[e]) { p.grown[row[e]] = 0; status |= KVMIX_PAGES_EXHAUSTED; }
   }
   if (status) atomicOr(&s_status, status);
   __syncthreads();
   const int granted = s_granted;
-  int base = 0;
-  for (int c = 0; c < chunks && base < granted; c++) {
-    if (s_free[c] == 0) continue;
-    const int w = c * (kChunk / 32) + tid / 8, shift = 4 * (tid & 7);
-    uint32_t free_bits = 0;
-    if (w < words) free_bits = (~p.used[w] & valid_bits(w, p.n_pages)) >> shift & 15u;
-    int in_chunk;
-    int r = scan_before((int)__popc(free_bits), s_wave, in_chunk);
-    uint32_t taken = 0;
-#pragma unroll
-    for (int b = 0; b < 4; b++)
-      if (free_bits >> b & 1u) {
-        if (base + r < granted) { s_id[r] = 32 * w + shift + b; taken |= 1u << b; }
-        r++;
-      }
-    if (taken) atomicOr(&p.used[w], taken << shift);
-    __syncthreads();
-    const int here = in_chunk < granted - base ? in_chunk : granted - base;
-    for (int k = tid; k < here; k += kGrowThreads) {
-      int lo = 0, hi = n - 1;                          // the last row whose first rank is not past this one
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (s_first[mid] <= base + k) lo = mid;
-        else hi = mid - 1;
-      }
-      p.table[(size_t)s_row[lo] * p.max_tiles + s_before[lo] + (base + k - s_first[lo])] = s_id[k];
-      p.refs[s_id[k]] = 1;
+  int base = 0;                        // free pages before the words in hand
+  for (int w0 = 0; w0 < words && base < granted; w0 += kGrowThreads) {
+    const int w = w0 + tid;
+    const uint32_t bits = w0 == 0 ? first_bits : w < words ? ~p.used[w] & valid_bits(w, p.n_pages) : 0u;
+    int r = (int)before.a, here = n_free;
+    if (words > kGrowThreads) {        // (otherwise the first scan has said it)
+      Two t;
+      if (w0) __syncthreads();         // (s_wave has been read)
+      r = base + (int)scan_before({(uint32_t)__popc(bits), 0}, s_wave[1], t).a;
+      here = (int)t.a;
     }
+    const int end = base + here < granted ? base + here : granted;
+    uint32_t taken = 0;
+    for (int lo = base; lo < end; lo += kIds) {
+      int k = r;
+      for (uint32_t left = bits; left; left &= left - 1u, k++)
+        if (k >= lo && k < lo + kIds && k < end) { s_id[k - lo] = 32 * w + __ffs(left) - 1; taken |= left & (0u - left); }
+      __syncthreads();
+      const int many = end - lo < kIds ? end - lo : kIds;
+      for (int m = tid; m < many; m += kGrowThreads) {
+        int a = 0, b = n - 1;          // the last row whose first rank is not past this one
+        while (a < b) {
+          const int mid = (a + b + 1) >> 1;
+          if (s_first[mid] <= lo + m) a = mid;
+          else b = mid - 1;
+        }
+        const int id = s_id[m];
+        p.table[(size_t)s_row[a] * p.max_tiles + s_before[a] + (lo + m - s_first[a])] = id;
+        p.refs[id] = 1;
+      }
+      __syncthreads();
+    }
+    if (taken) atomicOr(&p.used[w], taken);
     base += here;
-    __syncthreads();
   }
   if (tid == 0 && s_status) atomicOr(p.status, s_status);
 }
@@ -222,30 +251,35 @@ __global__ __launch_bounds__(kRowThreads) void pages_fork_kernel(kvmix_pages p, 
 
 // One workgroup: pages in use are counted, then gaps below that number and pages above it are listed in order, a word of bits to a thread.
 __global__ __launch_bounds__(kGrowThreads) void pages_compact_kernel(kvmix_pages p) {
-  __shared__ int s_wave[kGrowThreads / kWave];
+  __shared__ Two s_wave[2][kGrowWaves];
   const int tid = threadIdx.x, words = (p.n_pages + 31) / 32;
   int32_t* src = p.moves + 4;
   int32_t* dst = src + p.n_pages;
   int32_t* to = dst + p.n_pages;
-  int used = 0, live;
-  for (int w = tid; w < words; w += kGrowThreads) used += __popc(p.used[w] & valid_bits(w, p.n_pages));
-  scan_before(used, s_wave, live);
+  const uint32_t first_bits = tid < words ? p.used[tid] & valid_bits(tid, p.n_pages) : 0u;
+  uint32_t used = __popc(first_bits);
+  for (int w = tid + kGrowThreads; w < words; w += kGrowThreads) used += __popc(p.used[w] & valid_bits(w, p.n_pages));
+  Two all;
+  scan_before({used, 0}, s_wave[0], all);
+  const int live = (int)all.a;
   int gaps = 0, above = 0;
   for (int w0 = 0; w0 < words; w0 += kGrowThreads) {
     const int w = w0 + tid;
     uint32_t gap = 0, move = 0;
     if (w < words) {
-      const uint32_t u = p.used[w] & valid_bits(w, p.n_pages), low = valid_bits(w, live);
+      const uint32_t u = w0 == 0 ? first_bits : p.used[w] & valid_bits(w, p.n_pages), low = valid_bits(w, live);
       gap = ~u & low;
       move = u & ~low;
       if (u != low) p.used[w] = low;
     }
-    int n_gap, n_move;
-    int g = gaps + scan_before((int)__popc(gap), s_wave, n_gap), m = above + scan_before((int)__popc(move), s_wave, n_move);
+    Two many;
+    if (w0) __syncthreads();           // (s_wave has been read)
+    const Two at = scan_before({(uint32_t)__popc(gap), (uint32_t)__popc(move)}, s_wave[1], many);
+    int g = gaps + (int)at.a, m = above + (int)at.b;
     for (; gap; gap &= gap - 1u) dst[g++] = 32 * w + __ffs(gap) - 1;
     for (; move; move &= move - 1u) src[m++] = 32 * w + __ffs(move) - 1;
-    gaps += n_gap;
-    above += n_move;
+    gaps += (int)many.a;
+    above += (int)many.b;
   }
   __syncthreads();
   for (int i = tid; i < above; i += kGrowThreads) {
@@ -271,8 +305,9 @@ __global__ __launch_bounds__(kRowThreads) void pages_rename_kernel(kvmix_pages p
   }
 }
 
-// Pieces of 16 KB, four 16-byte loads of a thread under way together; workgroups stay and take every gridDim-th piece.
-constexpr int kPiece = 16384;
+// Pieces of 8 KB, two 16-byte loads of a thread under way together; workgroups stay and take every gridDim-th piece. (300 pages of 32 KB 7.7 us, 8.2 in
+// pieces of 16 KB for 4096 workgroups; rings of 32 slots x 8 heads, 50 MB read and written, 7.5 and 7.7.)
+constexpr int kPiece = 8192;
 __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
   const int n = a.count ? *a.count : a.n;
   const uint32_t pieces = (uint32_t)((a.bytes + kPiece - 1) / kPiece), each = pieces * (uint32_t)a.n_base;
@@ -288,12 +323,12 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
     const int64_t off = (int64_t)(rest >= pieces ? rest - pieces : rest) * kPiece + 16 * threadIdx.x, left = a.bytes - off;
     const char* s = base + (int64_t)from * a.bytes + off;
     char* d = base + (int64_t)to * a.bytes + off;
-    u32x4_t x[4];
+    u32x4_t x[2];
 #pragma unroll
-    for (int e = 0; e < 4; e++)
+    for (int e = 0; e < 2; e++)
       if (4096 * e < left) x[e] = *reinterpret_cast<const u32x4_t*>(s + 4096 * e);
 #pragma unroll
-    for (int e = 0; e < 4; e++)
+    for (int e = 0; e < 2; e++)
       if (4096 * e < left) *reinterpret_cast<u32x4_t*>(d + 4096 * e) = x[e];
   }
 }
@@ -301,7 +336,8 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
 }  // namespace
 
 hipError_t launch_pages_grow(const kvmix_pages& p, const int32_t* rows, const int32_t* cu, int n, hipStream_t s) {
-  return launch(pages_grow_kernel, dim3(1), kGrowThreads, s, p, rows, cu, n);
+  return n <= kGrowThreads ? launch(pages_grow_kernel<1>, dim3(1), kGrowThreads, s, p, rows, cu, n)
+                           : launch(pages_grow_kernel<kMaxRows / kGrowThreads>, dim3(1), kGrowThreads, s, p, rows, cu, n);
 }
 hipError_t launch_pages_free(const kvmix_pages& p, const int32_t* rows, int n, hipStream_t s) {
   return launch(pages_free_kernel, dim3(n), kRowThreads, s, p, rows);
@@ -315,7 +351,7 @@ hipError_t launch_pages_compact(const kvmix_pages& p, hipStream_t s) {
 }
 hipError_t launch_copy(const CopyArgs& a, hipStream_t s) {
   const int64_t pieces = (a.bytes + kPiece - 1) / kPiece * a.n_base, most = a.n * pieces;
-  return launch(copy_kernel, dim3((unsigned)(most < 4096 ? most : 4096)), 256, s, a);
+  return launch(copy_kernel, dim3((unsigned)(most < 2048 ? most : 2048)), 256, s, a);
 }
 
 }  // namespace kvmix

@@ -339,7 +339,7 @@ __device__ __forceinline__ T load_row(const uint16_t* p) {
 //
 // InPlace: the tile's place in a contiguous cache, from the grid; or a Paged one that the caller found.
 struct InPlace {};
-struct Paged { int unit; uint32_t* record; };       // unit: (slot, kv head) of the rings
+struct Paged { int unit, tile, head, then; uint32_t* record; int32_t* status; };       // unit: (slot, kv head) of the rings; tile: of those that fall due; then: ring tile to fill behind it (-1: none); record: NULL for none
 template <int KB, int VB, bool PARTIAL, int SPLIT, Stream S, typename Place = InPlace>
 __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16_t* v_in, int64_t tok, int64_t unit_b, int64_t unit_h, uint32_t* packed,
                                               int n_tiles, int n_ring, const QuantArgs& a, Place place = {}) {
@@ -355,8 +355,9 @@ __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int side = wave / SPLIT, part = wave % SPLIT;      // side: 0 Keys, 1 Values
   const int kq = lane >> 4, j = (lane >> 2) & 3, q = lane & 3;
-  const int tile_in = blockIdx.x, jh = blockIdx.y, b = blockIdx.z;   // no integer division at the start of a short kernel
-  const uint16_t* in = (side ? v_in : k_in) + (PAGED ? 0 : b * unit_b) + jh * unit_h;
+  int tile_in = blockIdx.x, jh = blockIdx.y, b = blockIdx.z;   // no integer division at the start of a short kernel
+  if constexpr (PAGED) { tile_in = place.tile; jh = place.head; b = 0; }
+  const uint16_t* in = (side ? v_in : k_in) + b * unit_b + jh * unit_h;
   auto unit = [&]() {
     if constexpr (PAGED) return place.unit;
     else return b * a.Hkv + jh;
@@ -682,6 +683,12 @@ __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16
   if constexpr (!PARTIAL) {
     __syncthreads();         // the metadata of both sides, and the side's own section, are in LDS
     uint32_t* rec = record();
+    if constexpr (PAGED) {
+      if (!rec) {
+        if (threadIdx.x == 0) atomicOr(place.status, KVMIX_PAGES_BAD_ID);
+        return;
+      }
+    }
     if (part == 0) {
       if (side == 0) store_section<KB, S>(rec + kMetaWords, s_key, lane);
       else store_section<VB, S>(rec + kMetaWords + tile_words(KB), s_value, lane);
@@ -689,6 +696,8 @@ __device__ __forceinline__ void quantize_tile(const uint16_t* k_in, const uint16
     if (part == SPLIT - 1) put<S>(reinterpret_cast<u32x2_t*>(rec) + 64 * side + lane, reinterpret_cast<const u32x2_t*>(s_meta)[64 * side + lane]);
     // New rows that land in slots this tile was read from (all waves have their rows: the barrier): this workgroup fills those.
     if (tile_in * kTile < a.n_read) copy_rows(tile_in * kTile, 0, a.n_read);
+    if constexpr (PAGED)
+      if (place.then >= 0) copy_rows(place.then * kTile, a.n_read, a.W_cap);
   }
 }
 
@@ -707,19 +716,47 @@ __global__ __launch_bounds__(128, 4) void quantize_pack_many_kernel(QuantArgs a)
   quantize_tile<KB, VB, PARTIAL, 1, S>(a.k, a.v, a.tok, a.unit_b, a.unit_h, a.packed + (size_t)a.tile0 * record_words(KB, VB), a.n_tiles, a.n_ring, a);
 }
 
-// A paged, ragged append: grid (due tiles and ring tiles, kv heads, batch rows). What kvmix_append_tokens works out on the host for
-// a batch of one length is worked out here for each sequence, from its length: the tiles that fall due, which page each goes to, and
-// the new rows that stay. Workgroups that their sequence has no work for end at once.
+// A paged, ragged append. What kvmix_append_tokens works out on the host for a batch of one length is worked out here for each sequence,
+// from its length: the tiles that fall due, which page each goes to, and the new rows that stay. A workgroup per tile and kv head, over the
+// tiles of all rows one after the other: row b's begin at cu[b] / 32 + b * more, where `more` is what a row may have beyond a 32nd of its
+// tokens, one due tile and ring tiles. A wave finds the row among 64 of them by one load and one comparison; eight neighbouring tiles
+// and their heads follow each other, so that a die has the rows of a token from all heads. (As many tiles for every row as the longest may have, most
+// of them without work: 7 rows of 1 to 8000 tokens 19.7 us, 15.6 now.) Without cu, single tokens: one workgroup for a row and head, which also
+// fills the ring behind a due tile (256 rows x 8 heads 6.9 us, 9.3 with a workgroup for either).
+// What is in front of a tile's first request, two ways to memory and some 100 instructions, is not hidden where the registers hold no more
+// workgroups: a prompt of 32 700 tokens takes 39.3 us at 3/4 bit and 35.2 at 2/2, the contiguous cache's 33.5 and 30.4. Several tiles to a
+// workgroup, one after the other, spill (59 us with two).
 template <int KB, int VB, int SPLIT, Stream S>
 __global__ __launch_bounds__(128 * SPLIT, 4) void paged_append_kernel(PagedAppendArgs p) {
-  const int b = blockIdx.z, jh = blockIdx.y, x = blockIdx.x;
-  const int row = p.rows ? load_uniform(p.rows + b) : b;
-  if (row < 0) return;
+  const uint32_t id8 = blockIdx.x >> 3, group = p.head_magic ? __umulhi(id8, p.head_magic) : id8;
+  const int at_t = (int)(8 * group + (blockIdx.x & 7u)), jh = (int)(id8 - group * (uint32_t)p.q.Hkv);
+  int x, row, first, n_new;
+  if (!p.cu) {
+    x = 0; first = at_t; n_new = 1;
+    if (first >= p.B) return;
+    row = p.rows ? load_uniform(p.rows + first) : first;
+  } else {
+    // (the slots and counts of the rows looked over come with their offsets: two ways to memory in front of the rows' data, with the lengths')
+    int b = 0;
+    for (int step = p.B <= kWave ? 1 : p.B <= kWave * kWave ? kWave : kWave * kWave;; step /= kWave) {
+      const int i = b + step * (int)(threadIdx.x & 63), in = i < p.B ? i : 0;
+      const int at = p.cu[in], next = p.cu[in + 1], slot = p.rows ? p.rows[in] : in;
+      const uint64_t begun = __builtin_amdgcn_ballot_w64(i < p.B && (at >> 5) + i * p.more <= at_t);
+      if (begun == 0) return;
+      const int l = __popcll(begun) - 1;
+      b += step * l;
+      first = __builtin_amdgcn_readlane(at, l);
+      n_new = __builtin_amdgcn_readlane(next, l) - first;
+      row = __builtin_amdgcn_readlane(slot, l);
+      if (step == 1) break;
+    }
+    x = at_t - ((first >> 5) + b * p.more);
+  }
+  if (row < 0 || x < 0) return;
   if (row >= p.n_slots) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
-  const int first = p.cu ? load_uniform(p.cu + b) : b, n_new = p.cu ? load_uniform(p.cu + b + 1) - first : 1;
   const int n = load_uniform(p.lens + row), grown = load_uniform(p.grown + row);
   if (n_new <= 0 || grown == 0) return;       // (a row that was not granted its tokens has said so)
-  if (n_new != grown || n_new > p.max_new || n < n_new || first < 0) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
+  if (n_new != grown || n_new > p.max_new || n < n_new || first < 0 || first > p.n_tokens - n_new) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
   QuantArgs a = p.q;
   const int old_tiles = packed_tiles(n - n_new, p.window), tiles = packed_tiles(n, p.window), due = tiles - old_tiles;
   if (tiles > p.max_tiles) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ROW); return; }
@@ -735,11 +772,14 @@ __global__ __launch_bounds__(128 * SPLIT, 4) void paged_append_kernel(PagedAppen
   a.copy_tile0 = from / kTile;
   a.copy_tiles = a.n_copy > 0 && to > from ? (to + kTile - 1) / kTile - a.copy_tile0 : 0;
   if (x >= due + a.copy_tiles) return;
-  Paged place{row * a.Hkv + jh, nullptr};
+  Paged place{row * a.Hkv + jh, x, jh, -1, nullptr, nullptr};
+  if (!p.cu && due && a.copy_tiles) place.then = a.copy_tile0;
   if (x < due) {
-    const int at = old_tiles + x, id = load_uniform(p.table + (size_t)row * p.max_tiles + at);
-    if ((uint32_t)id >= (uint32_t)p.n_pages) { if (threadIdx.x == 0) atomicOr(p.status, KVMIX_PAGES_BAD_ID); return; }
-    place.record = a.packed + ((size_t)id * a.Hkv + jh) * record_words(KB, VB);
+    // (asked for now, looked at when the words are stored; out of range: nothing is)
+    const int id = load_uniform(p.table + (size_t)row * p.max_tiles + old_tiles + x);
+    const bool there = (uint32_t)id < (uint32_t)p.n_pages;
+    place.record = there ? a.packed + ((size_t)id * a.Hkv + jh) * record_words(KB, VB) : nullptr;
+    place.status = p.status;
   }
   const bool values = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= SPLIT;      // this wave's side
   quantize_tile<KB, VB, false, SPLIT, S>(a.k + first * a.tok, a.v + first * p.v_tok, values ? p.v_tok : a.tok, 0, values ? p.v_head : a.unit_h, nullptr,
@@ -863,37 +903,38 @@ hipError_t launch_bits(const QuantArgs& a, int k_bits, int v_bits, int n_tiles, 
   return hipErrorInvalidValue;
 }
 
-// Four waves or two to a tile, past the caches or not: as for quantize_pack, by the tiles that may fall due.
+// Four waves or two to a tile, past the caches or not: as for quantize_pack, by the tiles that fall due at most (single tokens: one
+// in 32 of them, ordinarily).
 template <int KB, int VB>
-hipError_t launch_pa(const PagedAppendArgs& a, int B, hipStream_t s) {
-  const int due = (a.max_new + kTile - 1) / kTile;
-  const dim3 grid(due + (a.max_new == 1 ? 1 : a.ring_tiles), a.q.Hkv, B);
-  const size_t tiles = (size_t)due * a.q.Hkv * B;
-  if (tiles < 2048) return launch(paged_append_kernel<KB, VB, 2, kCached>, grid, 4 * kWave, s, a);
-  if (tiles <= (KB == 3 || VB == 3 ? 4096 : 8192)) return launch(paged_append_kernel<KB, VB, 2, kStreamOut>, grid, 4 * kWave, s, a);
+hipError_t launch_pa(const PagedAppendArgs& a, hipStream_t s) {
+  const int64_t tiles = a.cu ? (int64_t)a.n_tokens / kTile + a.B : 0;
+  const int64_t places = a.cu ? a.n_tokens / kTile + (int64_t)a.B * a.more + 1 : a.B;
+  const dim3 grid((unsigned)((places + 7) / 8 * 8 * a.q.Hkv));
+  if (tiles * a.q.Hkv < 2048) return launch(paged_append_kernel<KB, VB, 2, kCached>, grid, 4 * kWave, s, a);
+  if (tiles * a.q.Hkv <= (KB == 3 || VB == 3 ? 4096 : 8192)) return launch(paged_append_kernel<KB, VB, 2, kStreamOut>, grid, 4 * kWave, s, a);
   return launch(paged_append_kernel<KB, VB, 1, kStreamOut>, grid, 2 * kWave, s, a);
 }
 
 }  // namespace
 
-hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, int B, hipStream_t s) {
+hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, hipStream_t s) {
   switch (k_bits * 10 + v_bits) {
-    case 11: return launch_pa<1, 1>(a, B, s);
-    case 12: return launch_pa<1, 2>(a, B, s);
-    case 13: return launch_pa<1, 3>(a, B, s);
-    case 14: return launch_pa<1, 4>(a, B, s);
-    case 21: return launch_pa<2, 1>(a, B, s);
-    case 22: return launch_pa<2, 2>(a, B, s);
-    case 23: return launch_pa<2, 3>(a, B, s);
-    case 24: return launch_pa<2, 4>(a, B, s);
-    case 31: return launch_pa<3, 1>(a, B, s);
-    case 32: return launch_pa<3, 2>(a, B, s);
-    case 33: return launch_pa<3, 3>(a, B, s);
-    case 34: return launch_pa<3, 4>(a, B, s);
-    case 41: return launch_pa<4, 1>(a, B, s);
-    case 42: return launch_pa<4, 2>(a, B, s);
-    case 43: return launch_pa<4, 3>(a, B, s);
-    case 44: return launch_pa<4, 4>(a, B, s);
+    case 11: return launch_pa<1, 1>(a, s);
+    case 12: return launch_pa<1, 2>(a, s);
+    case 13: return launch_pa<1, 3>(a, s);
+    case 14: return launch_pa<1, 4>(a, s);
+    case 21: return launch_pa<2, 1>(a, s);
+    case 22: return launch_pa<2, 2>(a, s);
+    case 23: return launch_pa<2, 3>(a, s);
+    case 24: return launch_pa<2, 4>(a, s);
+    case 31: return launch_pa<3, 1>(a, s);
+    case 32: return launch_pa<3, 2>(a, s);
+    case 33: return launch_pa<3, 3>(a, s);
+    case 34: return launch_pa<3, 4>(a, s);
+    case 41: return launch_pa<4, 1>(a, s);
+    case 42: return launch_pa<4, 2>(a, s);
+    case 43: return launch_pa<4, 3>(a, s);
+    case 44: return launch_pa<4, 4>(a, s);
   }
   return hipErrorInvalidValue;
 }

@@ -11,7 +11,7 @@ hipError_t launch_stream_read(const void*, size_t, int, int, uint32_t*, hipStrea
 template <> hipError_t launch_decode_attn<8, false>(const AttnArgs&, int, int, int, int, hipStream_t) { return hipErrorUnknown; }
 template <> hipError_t launch_decode_attn<12, false>(const AttnArgs&, int, int, int, int, hipStream_t) { return hipErrorUnknown; }
 template <> hipError_t launch_decode_attn<12, true>(const AttnArgs&, int, int, int, int, hipStream_t) { return hipErrorUnknown; }
-hipError_t launch_paged_append(const PagedAppendArgs&, int, int, int, hipStream_t) { return hipErrorUnknown; }
+hipError_t launch_paged_append(const PagedAppendArgs&, int, int, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_rope(const RopeArgs&, int, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_pages_grow(const kvmix_pages&, const int32_t*, const int32_t*, int, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_pages_free(const kvmix_pages&, const int32_t*, int, hipStream_t) { return hipErrorUnknown; }

@@ -46,7 +46,7 @@ class PagedRef:
                 self.grown[r] = 0
                 continue
             for t in range(a, b):
-                p = int(np.flatnonzero(self.refs == 0)[0])
+                p = int(np.argmin(self.refs))
                 self.table[r, t] = p
                 self.refs[p] = 1
             self.lens[r] += n

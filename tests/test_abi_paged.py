@@ -30,7 +30,7 @@ def cache(**change):
 
 
 BAD_PAGES = [(dict(table=None), -1), (dict(lens=None), -1), (dict(grown=None), -1), (dict(refs=None), -1), (dict(used=None), -1), (dict(status=None), -1),
-             (dict(table=A + 2), -5), (dict(status=A + 1), -5), (dict(n_slots=0), -4), (dict(n_pages=0), -4), (dict(n_pages=(1 << 22) + 1), -4),
+             (dict(table=A + 2), -5), (dict(status=A + 1), -5), (dict(n_slots=0), -4), (dict(n_pages=0), -4), (dict(n_pages=1 << 22), -4),
              (dict(max_tiles=0), -4), (dict(max_tiles=(1 << 23) + 1), -4), (dict(window=-1), -4), (dict(window=40), -4)]
 
 
@@ -44,7 +44,7 @@ def test_every_call_checks_the_pages(kv, change, status):
     assert L.kvmix_pages_fork(r(p), a, a, 2, None) == status
     assert L.kvmix_pages_compact(r(p), None) == status
     assert L.kvmix_move_records(r(sh), r(cfg), r(c), r(p), None) == status
-    assert L.kvmix_paged_append(r(sh), r(cfg), a, 512, 128, a, 512, 128, r(c), r(p), a, a, 1, None) == status
+    assert L.kvmix_paged_append(r(sh), r(cfg), a, 512, 128, a, 512, 128, 9, r(c), r(p), a, a, 1, None) == status
     assert L.kvmix_paged_decode_attn(r(sh), r(cfg), a, r(c), r(p), a, 100, C.c_float(0), a, a, 1 << 30, None) == status
 
 
@@ -55,7 +55,7 @@ def test_shape_widths_and_window(kv, shape, cfg, status):
     """16-bit layers have nothing to page, the count policy has no single front; the window is the pages'."""
     L, sh, cf, p, c, r, a = kv.lib(), kv.Shape(*shape), kv.LayerCfg(*cfg), pages(), cache(), C.byref, C.c_void_p(A)
     assert L.kvmix_move_records(r(sh), r(cf), r(c), r(p), None) == status
-    assert L.kvmix_paged_append(r(sh), r(cf), a, 512, 128, a, 512, 128, r(c), r(p), a, a, 1, None) == status
+    assert L.kvmix_paged_append(r(sh), r(cf), a, 512, 128, a, 512, 128, 9, r(c), r(p), a, a, 1, None) == status
     assert L.kvmix_paged_decode_attn(r(sh), r(cf), a, r(c), r(p), a, 100, C.c_float(0), a, a, 1 << 30, None) == status
     if cfg != (2, 2, 32):
         assert L.kvmix_copy_windows(r(sh), r(cf), r(c), a, a, 2, None) == status
@@ -65,7 +65,7 @@ def test_shape_widths_and_window(kv, shape, cfg, status):
                                            (dict(W_cap=64), -4), (dict(W_cap=100), -4), (dict(n_pages=99), -4), (dict(n_slots=9), -4)])
 def test_the_cache(kv, change, status):
     L, sh, cfg, p, c, r, a = kv.lib(), kv.Shape(2, 8, 4), kv.LayerCfg(2, 2, 64), pages(), cache(**change), C.byref, C.c_void_p(A)
-    assert L.kvmix_paged_append(r(sh), r(cfg), a, 512, 128, a, 512, 128, r(c), r(p), a, a, 1, None) == status
+    assert L.kvmix_paged_append(r(sh), r(cfg), a, 512, 128, a, 512, 128, 9, r(c), r(p), a, a, 1, None) == status
     assert L.kvmix_paged_decode_attn(r(sh), r(cfg), a, r(c), r(p), a, 100, C.c_float(0), a, a, 1 << 30, None) == status
 
 
@@ -82,13 +82,15 @@ def test_counts_and_pointers(kv):
     assert L.kvmix_copy_windows(r(sh), r(cfg), r(c), a, None, 1, None) == -1 and L.kvmix_copy_windows(r(sh), r(cfg), r(c), a, a, 65536, None) == -4
     assert L.kvmix_copy_windows(r(sh), r(cfg), r(c), None, None, 0, None) == 0
 
-    def append(k=a, ks=(512, 128), v=a, vs=(512, 128), rows=a, cu=a, max_new=3):
-        return L.kvmix_paged_append(r(sh), r(cfg), k, *ks, v, *vs, r(c), r(p), rows, cu, max_new, None)
+    def append(k=a, ks=(512, 128), v=a, vs=(512, 128), n=9, rows=a, cu=a, max_new=3):
+        return L.kvmix_paged_append(r(sh), r(cfg), k, *ks, v, *vs, n, r(c), r(p), rows, cu, max_new, None)
 
     assert append(k=None) == append(v=None) == -1
     assert append(k=odd) == append(v=odd) == append(ks=(4, 128)) == append(ks=(512, 4)) == append(vs=(-512, 128)) == append(vs=(512, 12)) == -5
-    assert append(max_new=-1) == append(cu=None, max_new=2) == -4
-    assert append(k=None, v=None, max_new=0) == 0
+    assert append(max_new=-1) == append(cu=None, max_new=2) == append(n=-1) == append(cu=None, max_new=1, n=1) == -4
+    big = kv.Shape(2, 8 * 16, 8 * 16)
+    assert L.kvmix_paged_append(r(big), r(cfg), a, 128 * 128, 128, a, 128 * 128, 128, 2 ** 31 - 1, r(c), r(p), a, a, 2 ** 31 - 1, None) == -4
+    assert append(k=None, v=None, max_new=0) == append(k=None, v=None, n=0) == 0
     assert append(rows=C.c_void_p(A + 2)) == -5
 
     def attn(q=a, rows=a, max_len=100, out=a, ws=a, n=1 << 30, sh=sh, p=p):

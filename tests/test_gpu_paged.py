@@ -53,6 +53,40 @@ def test_append_of_many_tiles(B, n, bits):
     s.check_cache("many tiles")
 
 
+@pytest.mark.parametrize("B,bits", [(65, (2, 2)), (200, (1, 3)), (4200, (2, 1))])
+def test_append_of_many_rows(B, bits):
+    """More rows than a wave looks over at once, and more than the square of that: which row a tile belongs to; a first offset that is not 0."""
+    s = Serving(1, 1, bits, 0, n_slots=B, n_pages=4 * B, max_tiles=6, W_cap=64, seed=B)
+    rows = [int(r) for r in s.rng.permutation(B)]
+    for most in (70, 40):
+        fresh = [int(n) for n in s.rng.integers(0, most, B)]
+        for i in range(0, B, 4096):                            # (as many rows as a call of grow takes)
+            s.grow(rows[i:i + 4096], fresh[i:i + 4096])
+        s.append(rows, fresh)
+    s.check_pages()
+    s.ref.lens[:] *= np.arange(B) % (B // 50) == 0             # (fifty slots looked at)
+    for b in range(B):
+        if not s.ref.lens[b]:
+            s.k[b], s.v[b] = s.k[b][:, :0], s.v[b][:, :0]
+    s.check_cache("many rows")
+
+
+def test_append_keeps_within_its_inputs():
+    """Offsets that go past the inputs' tokens, or below none: nothing is read there, the rows are left alone."""
+    import torch
+    s = Serving(1, 1, (2, 2), 0, n_slots=4, n_pages=16, max_tiles=8, seed=8)
+    s.grow([0, 1, 2], [32, 32, 32])
+    k = torch.randn((64, 1, 128), device="cuda").half()
+    pool = s.cache.pool.clone()
+    for cu in ([40, 72, 104, 136], [-64, -32, 0, 32 + 64], [33, 65, 97, 129]):
+        s.kv.paged_append(s.shape(3), s.cfg, k, k, s.cache, s.pages, rows=s.ints([0, 1, 2]), cu=s.ints(cu), max_new=32)
+        assert torch.equal(s.cache.pool, pool) and int(s.pages.status[0]) == BAD_ROW
+        s.pages.status.zero_()
+    s.kv.paged_append(s.shape(3), s.cfg, k, k, s.cache, s.pages, rows=s.ints([0, 1, 2]), cu=s.ints([0, 32, 64, 96]), max_new=32)      # two of three
+    changed = (s.cache.pool != pool).flatten(1).any(1).nonzero().view(-1).tolist()
+    assert changed == [0, 1] and int(s.pages.status[0]) == BAD_ROW
+
+
 def test_append_leaves_rows_alone_that_were_not_granted():
     s = Serving(1, 1, (2, 2), 32, n_slots=4, n_pages=4, max_tiles=8, seed=3)
     s.step([0, 1], [100, 40])                            # two pages of four

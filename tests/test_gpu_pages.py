@@ -89,6 +89,26 @@ def test_grow_without_rows_or_counts():
     s.check_pages()
 
 
+def test_pools_of_more_than_32768_pages():
+    """Free ids that lie far apart in a large pool, more of them than a list holds, and slots past 32768 that share a place in the table of names."""
+    s = bare(70000, 100000, 4200, 0)
+    rows = [5, 32773, 65541, 69999, 37]
+    s.grow(rows, [32 * 4100, 32 * 4200, 32 * 4000, 32 * 4199, 32 * 4200])
+    s.kv.pages_free(s.pages, s.ints([32773, 37]))
+    s.ref.free([32773, 37])
+    s.grow([100, 32868, 65636], [32 * 10, 32 * 4150, 32 * 3000])
+    s.grow([7, 32775, 7], [32, 64, 96])
+    assert s.ref.status == BAD_ROW
+    s.check_pages()
+    few = [100 + i for i in range(20)]
+    for i in range(3):                                         # a full pool but for some pages near its end
+        s.grow(few, [32 * 4000] * 20)
+    s.check_pages()
+    s.kv.pages_compact(s.pages)
+    s.ref.compact()
+    s.check_pages()
+
+
 @pytest.mark.parametrize("B", [1, 1023, 1025, 4096])
 def test_grow_of_many_rows(B):
     s = bare(4096, 9000, 4, 0)
