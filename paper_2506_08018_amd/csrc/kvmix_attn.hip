@@ -474,9 +474,37 @@ __device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* 
   Piece p = {};
   p.row = -1;
   p.total = choice == 3 ? here : total >> (10 * choice) & 1023;
+  if (k >= p.total) return p;
+  if constexpr (N == 1) {
+    // Large pieces first, by eighths of the largest: what is dispatched last is small. Where all are resident, and some compute units
+    // have two, the small ones go with large ones: workgroups are placed unit after unit (as far as can be told), so that the k-th meets the
+    // (k + units)-th.
+    const int n = choice == 3 ? (slot[0] >= 0 ? 1 : 0) : cuts[0] >> (10 * choice) & 1023;
+    const float eighths = 8.0f * __builtin_amdgcn_rcpf(fmaxf(fminf(share[choice], most), 1.0f));
+    const int size = n == 0 ? -1 : (int)fminf(units[0] * __builtin_amdgcn_rcpf((float)n) * eighths, 7.0f);
+    int rank = 0, ahead = 0;
+#pragma unroll
+    for (int c = 7; c >= -1; c--) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(size == c);
+      const int at = ahead + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+      rank = size == c ? at : rank;
+      ahead += __popcll(m);
+    }
+    const int sorted = __builtin_amdgcn_ds_permute(4 * rank, lane << 10 | n), up = wave_scan(sorted & 1023);
+    const int units_each = (int)(0.5f * a.places * __builtin_amdgcn_rcpf(groups)), second = p.total - units_each;
+    if (second > 0 && second <= units_each) k = k >= units_each ? p.total - 1 - (k - units_each) : k < second ? k + units_each - second : k - second;
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(k < up));
+    const int picked = __builtin_amdgcn_readlane(sorted, at), l = picked >> 10;
+    p.row = l;
+    p.slot = __builtin_amdgcn_readlane(slot[0], l);
+    p.len = __builtin_amdgcn_readlane(len[0], l);
+    p.splits = picked & 1023;
+    p.first = __builtin_amdgcn_readlane(up, at) - p.splits;
+    p.sp = k - p.first;
+  }
   int before = 0;
 #pragma unroll
-  for (int r = 0; r < N; r++) {
+  for (int r = 0; r < (N == 1 ? 0 : N); r++) {
     const uint64_t there = __builtin_amdgcn_ballot_w64(slot[r] >= 0);
     const int n = choice == 3 ? (slot[r] >= 0 ? 1 : 0) : cuts[r] >> (10 * choice) & 1023;
     const int up = choice == 3 ? before + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0)) + n
@@ -493,7 +521,6 @@ __device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* 
     }
     before += __popcll(there);
   }
-  if (p.row < 0) return p;
   // as plan_attention deals a context out
   const int n = p.len < 0 ? 0 : p.len;
   p.tiles = packed_tiles(n, a.window);
