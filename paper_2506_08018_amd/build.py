@@ -23,6 +23,7 @@ OBJECTS = {
     "kvmix_attn12.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=0", "-DKVMIX_PAGED=0"]),
     "kvmix_attn12_fronts.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=1", "-DKVMIX_PAGED=0"]),
     "kvmix_attn8_paged.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=8", "-DKVMIX_MIXED=0", "-DKVMIX_PAGED=1"]),
+    "kvmix_attn12_paged.o": ("kvmix_attn.hip", ATTN + ["-DKVMIX_WAVES=12", "-DKVMIX_MIXED=0", "-DKVMIX_PAGED=1"]),
     "kvmix_pages.o": ("kvmix_pages.hip", []),
     "kvmix_rope.o": ("kvmix_rope.hip", []),
     "kvmix_api.o": ("kvmix_api.hip", []),

@@ -604,9 +604,10 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     jh = (int)blockIdx.x; at_blk = 0;
     if (a.head_blocks > 1) { jh = (int)blockIdx.x / a.head_blocks; at_blk = (int)blockIdx.x - jh * a.head_blocks; }
     float workgroups = 0.0f;
-    if (n_rows == 1) {
+    constexpr bool kOneRow = NW == 12;      // (the form of 12 waves is for one long context)
+    if (kOneRow || n_rows == 1) {
       // One sequence: shares of the size that suits max_len (the host's), so that the page ids and the length are on their way together
-      // (as a piece of a batch: one small layer 6.3 -> 7.6 us, 8 units x 2048 tokens 6.9 -> 8.2).
+      // (as a piece of a batch one small layer takes 7.6 us, 6.6 this way, 8 units x 2048 tokens 8.2 and 7.1).
       const int slot = rows ? load_uniform(rows) : 0;
       if ((uint32_t)slot >= (uint32_t)a.n_slots) return;
       id_row = word_ptr(items[0], items[1]) + (size_t)slot * n_ids;
@@ -624,7 +625,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
       a.items_q = a.share; a.items_r = 0; a.win_tiles = 0;
       part_row = (size_t)jh * a.n_splits;
       workgroups = (float)a.n_splits * a.groups;
-    } else {
+    } else if constexpr (!kOneRow) {
       __shared__ Piece s_piece;
       if (wave == 0) {
         const Piece p = n_rows <= kWave ? find_piece<1>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
@@ -682,7 +683,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   if constexpr (PAGED) {
     if (last > tiles) last = tiles;                // (the last share of one sequence)
     ids_at = first;
-    if ((items[3] & 1023u) != 1u) ids = load_ids();
+    if (NW != 12 && (items[3] & 1023u) != 1u) ids = load_ids();
   }
 
   // ---- the query and the wave's first tile are requested before anything else is done.
@@ -1983,8 +1984,10 @@ hipError_t launch_g(const PagedAttnArgs& a, u32x4_t shares, u32x4_t items, int b
     case 1: return run(decode_attn_kernel<KB, VB, 1, kNW, false, true>);
     case 2: return run(decode_attn_kernel<KB, VB, 2, kNW, false, true>);
     case 4: return run(decode_attn_kernel<KB, VB, 4, kNW, false, true>);
-    case 8: if constexpr (VB < 3) return run(decode_attn_kernel<KB, VB, 8, kNW, false, true>); break;
+    case 8: if constexpr (kNW == 12 || VB < 3) return run(decode_attn_kernel<KB, VB, 8, kNW, false, true>); break;
+#if KVMIX_WAVES == 8
     case 16: return run(decode_attn_kernel<KB, VB, 16, kNW, false, true>);
+#endif
   }
   return hipErrorInvalidValue;
 }
@@ -2017,7 +2020,8 @@ hipError_t launch_decode_attn<kNW, kMixed>(const AttnArgs& a, int k_bits, int v_
   return hipErrorInvalidValue;
 }
 #else
-hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s) {
+template <>
+hipError_t launch_paged_attn<kNW>(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s) {
   const dim3 grid(a.Hkv * a.head_blocks, pieces);
   auto words = [](const int32_t* x, const int32_t* y) {
     const uint64_t p = reinterpret_cast<uint64_t>(x), q = reinterpret_cast<uint64_t>(y);

@@ -172,7 +172,7 @@ __host__ __device__ __forceinline__ float model_time(float workgroups, float lar
          : workgroups <= places      ? largest + kFixedTiles
                                      : fair + kFixedTiles * workgroups * inv_places + largest;
 }
-constexpr float kShares[3] = {1.1f, 1.5f, 2.2f};      // shares tried, besides whole contexts: times what each of `places` would get
+constexpr float kShares[3] = {1.1f, 1.5f, 2.2f};      // shares of a batch that are tried, besides whole contexts: times what each of `places` would get
 struct PagedAttnArgs : AttnArgs {
   int n_slots, n_pages, Hkv, window, max_len;
   float groups;           // workgroups of a piece: kv heads x blocks of heads
@@ -251,7 +251,11 @@ template <> hipError_t launch_decode_attn<12, false>(const AttnArgs& a, int k_bi
 template <> hipError_t launch_decode_attn<12, true>(const AttnArgs& a, int k_bits, int v_bits, int block, int units, hipStream_t s);
 
 
+// WAVES: 8, or 12 for one row (blocks of up to 8 heads)
+template <int WAVES>
 hipError_t launch_paged_attn(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s);
+template <> hipError_t launch_paged_attn<8>(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s);
+template <> hipError_t launch_paged_attn<12>(const PagedAttnArgs& a, const kvmix_pages& pages, const int32_t* rows, int n_rows, int pieces, int k_bits, int v_bits, int block, hipStream_t s);
 hipError_t launch_paged_append(const PagedAppendArgs& a, int k_bits, int v_bits, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t s);
 hipError_t launch_pages_grow(const kvmix_pages& p, const int32_t* rows, const int32_t* cu, int n, hipStream_t s);

@@ -47,7 +47,8 @@ uint32_t ring_magic(int ring_tiles) { return ring_tiles == 1 ? 0u : (uint32_t)((
 // workgroups that the chip holds at once (8 waves, two to a compute unit), so that there are at most kPlaces / (kv heads x head blocks)
 // pieces and one more for every row.
 constexpr int kRows = 512, kCus = 256, kPlaces = 2 * kCus;
-struct PagedPlan { int block, head_blocks, rows, pieces, share; size_t counters, bytes; };
+constexpr float kAloneInTwelve = 0.55f;       // kAlone of a workgroup of 12 waves
+struct PagedPlan { int block, head_blocks, rows, pieces, share, waves; size_t counters, bytes; };
 PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits) {
   PagedPlan p;
   const int G = sh->Hq / sh->Hkv;
@@ -61,20 +62,26 @@ PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits)
   p.pieces = (int)(by_places < by_length ? by_places : by_length);
   p.counters = ((size_t)p.rows * sh->Hkv * (G > 8 ? G / 8 : 1) * 4 + 255) / 256 * 256;
   p.bytes = p.counters + (size_t)p.pieces * sh->Hkv * G * (kD + 2) * sizeof(float);
-  p.share = 1;
+  p.share = 1; p.waves = 8;
   if (sh->B == 1) {
-    // (one sequence: the share that suits max_len, chosen as the device chooses a batch's)
+    // One sequence: unsplit, one workgroup or two to a compute unit, at most 64 pieces (1 x 8 heads over 32k tokens: 64 pieces 13.0 us, 256
+    // 17.0), by the model of a batch's launch. One to a compute unit has 12 waves where there are more than 20 tiles for it: 8 x 4 heads over
+    // 32k tokens 12.5 us (2/2 bit; 3/4 bit 13.3), 8 waves 13.4 (14.6), two of 8 waves 15.7 (16.5); over 120k tokens 23.9, 28.4, 25.2; 8 x 8
+    // heads at 2/4 bit over 32k 14.5, 17.1, 22.5; 8 x 2 heads over 16k, 16 tiles each, 9.85, 9.75, 11.8.
     const int groups = sh->Hkv * p.head_blocks;
-    const float fair = (float)most * groups / kPlaces;
     float best = INFINITY;
     int splits = 1;
-    for (int c = 3; c >= 0; c--) {
-      const float share = c == 3 ? (float)most : std::fmax(std::ceil(fair * kShares[c]), (float)kMinShare);
-      const float n = c == 3 ? 1.0f : std::fmax(std::ceil((float)most / share), 1.0f);
-      const float time = (n > 1.0f ? kMergeTiles * n : 0.0f) + model_time(n * groups, std::fmin(share, (float)most), fair, kPlaces, 1.0f / kPlaces);
-      if (time < best) { best = time; splits = (int)n; }
+    for (int places = 0; places <= kPlaces; places += kCus) {
+      int n = places / groups < 64 ? places / groups : 64;
+      if (n > p.pieces) n = p.pieces;
+      if (n < 1) n = 1;
+      const float largest = (float)((most + n - 1) / n);
+      const bool twelve = G <= 8 && (long long)n * groups <= kCus && tiles > 20 * n;
+      const float time = (n > 1 ? kMergeTiles * (float)n : 0.0f) + (twelve ? kAloneInTwelve / kAlone : 1.0f) *
+                         model_time((float)(n * groups), largest, (float)most * groups / kPlaces, kPlaces, 1.0f / kPlaces);
+      if (time < best) { best = time; splits = n; p.waves = twelve ? 12 : 8; }
     }
-    if (splits > p.pieces) splits = p.pieces;
+    if (p.waves == 12) p.block = G;
     p.share = tiles > splits ? (tiles + splits - 1) / splits : 1;
     p.pieces = tiles > 0 ? (tiles + p.share - 1) / p.share : 1;
   }
@@ -270,7 +277,8 @@ int kvmix_paged_decode_attn(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, c
     a.q = q + (size_t)b * sh->Hq * kD; a.out = out + (size_t)b * sh->Hq * kD;
     kvmix_pages here = *p;
     if (!rows) { here.table += (size_t)b * p->max_tiles; here.lens += b; a.k_win = c->k_win + (size_t)b * sh->Hkv * c->W_cap * kD; a.v_win = c->v_win + (size_t)b * sh->Hkv * c->W_cap * kD; a.n_slots = p->n_slots - b; }
-    const hipError_t e = launch_paged_attn(a, here, rows ? rows + b : nullptr, n, plan.pieces, cfg->k_bits, cfg->v_bits, plan.block, (hipStream_t)stream);
+    const auto run = plan.waves == 12 ? launch_paged_attn<12> : launch_paged_attn<8>;
+    const hipError_t e = run(a, here, rows ? rows + b : nullptr, n, plan.pieces, cfg->k_bits, cfg->v_bits, plan.block, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e);
   }
   return KVMIX_OK;

@@ -105,7 +105,7 @@ def test_counts_and_pointers(kv):
 @pytest.fixture(scope="module")
 def plan(tmp_path_factory):
     """kvmix_paged_decode_attn with its launch taken down: (B, Hkv, G, v_bits, W, max_len, workspace) -> status and, of the last
-    launch, pieces, batch rows, heads per block, bytes of counters, tiles of a share of one sequence."""
+    launch, pieces, batch rows, heads per block, bytes of counters, tiles of a share of one sequence, waves."""
     import os
     import subprocess
     from paper_2506_08018_amd import build
@@ -116,7 +116,7 @@ def plan(tmp_path_factory):
     f.argtypes = [C.c_int] * 6 + [C.c_size_t, C.c_void_p]
 
     def run(*args):
-        out = (C.c_longlong * 5)()
+        out = (C.c_longlong * 6)()
         return (f(*args, out), *out)
 
     return run
@@ -133,7 +133,7 @@ def test_workspace_is_enough_for_every_window_and_width(kv, plan):
             for W in (0, 32, 64, 256, 4096):
                 for vb in (2, 3):
                     for m in {n, max(1, n // 2), max(1, n - 33)}:
-                        st, pieces, rows, block, counters, _ = plan(B, Hkv, G, vb, W, m, need)
+                        st, pieces, rows, block, counters, _, _ = plan(B, Hkv, G, vb, W, m, need)
                         assert st == 0, (B, Hkv, G, n, W, vb, m)
                         assert pieces <= min(B, 512) or counters + pieces * Hkv * G * 520 <= need
 
@@ -151,12 +151,12 @@ def pieces_of(lens, W, places_scale, share):
 def test_the_grid_holds_every_piece(kv, plan):
     """However the lengths are spread below max_len, the pieces that they make are no more than the launch has workgroups for."""
     rng = np.random.default_rng(1)
-    for B, Hkv, G in [(1, 1, 1), (1, 8, 4), (2, 16, 1), (5, 2, 16), (64, 8, 8), (300, 1, 4), (512, 32, 1), (2, 1, 72), (7, 600, 1)]:
+    for B, Hkv, G in [(1, 1, 1), (1, 8, 4), (1, 40, 8), (1, 300, 2), (1, 1, 72), (2, 16, 1), (5, 2, 16), (64, 8, 8), (300, 1, 4), (512, 32, 1), (2, 1, 72), (7, 600, 1)]:
         for max_len in (1, 33, 95, 300, 5000, 70000, 2000000):
             for W in (0, 32, 256):
                 need = kv.paged_workspace_bytes(kv.Shape(B, G * Hkv, Hkv), max_len)
-                st, pieces, rows, block, _, share = plan(B, Hkv, G, 2, W, max_len, need)
-                assert st == 0 and rows == B
+                st, pieces, rows, block, _, share, waves = plan(B, Hkv, G, 2, W, max_len, need)
+                assert st == 0 and rows == B and (waves == 8 or (B == 1 and block == G <= 8))
                 HH = Hkv * -(-G // block)
                 for lens in ([max_len] * B, [max_len] + [0] * (B - 1), [max_len] + [1] * (B - 1), rng.integers(0, max_len + 1, B).tolist(),
                              np.exp(rng.uniform(0, np.log(max_len + 1), B)).astype(int).tolist(), [max(0, max_len - 31)] * B):

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from gpu_common import t16
+from gpu_common import assert_attn_close, t16
 from paged_common import Serving
 from paged_ref import BAD_ID, BAD_ROW, EXHAUSTED, one_sequence, tiles_of
 
@@ -169,6 +169,37 @@ def test_long_contexts_in_many_splits(G):
     s.check_attention([3, 3, 0, -1], "shorter ones next", ws=ws, max_len=32 * 500 + 32)
     if G <= 4:
         assert not ws.any()
+
+
+@pytest.mark.parametrize("bits", [(kb, vb) for kb in (1, 2, 3, 4) for vb in (1, 2, 3, 4)])
+def test_one_sequence_in_workgroups_of_twelve_waves(bits):
+    """One row with more than 20 tiles for each compute unit that it gets: the other form of the kernel, every width and group size; a shorter sequence
+    than max_len, an empty one and a padding row in the same form. Some heads against the oracle, the others against a batch of two."""
+    import torch
+    Hkv = 128
+    s = Serving(Hkv, 1, bits, 32, n_slots=3, n_pages=70, max_tiles=60, seed=20 + bits[0])
+    s.step([2, 0], [1429, 77])
+    for G in (1, 2, 4, 8):
+        s.G = G
+        q = s.rng.standard_normal((1, G * Hkv, 128), dtype=np.float32).astype(np.float16)
+        ws = torch.zeros(s.kv.paged_workspace_bytes(s.shape(2), 1800), dtype=torch.uint8, device="cuda")
+
+        def run(rows, max_len):
+            qt = torch.from_numpy(np.repeat(q, len(rows), 0)).cuda()
+            out = torch.full_like(qt, 7.0)
+            ws.zero_()
+            s.kv.paged_decode_attn(s.shape(len(rows)), s.cfg, qt, s.cache, s.pages, out, ws, rows=s.ints(rows), max_len=max_len)
+            torch.cuda.synchronize()
+            return out
+        both = run([2, 0], 1800)
+        for row, want in ((2, both[0]), (0, both[1])):
+            got = run([row], 1429)[0]
+            assert (got.float() - want.float()).abs().max().item() <= 4e-3, (G, row)      # (an fp16 spacing below 4: sums in another order)
+            heads = [0, 5, Hkv - 1]
+            st, ref = one_sequence(s.k[row][heads], s.v[row][heads], *bits, 32, G).decode_attn(q.reshape(1, Hkv, G, 128)[:, heads].reshape(1, -1, 128).view(np.uint16))
+            assert st == 0
+            assert_attn_close(t16(got).reshape(Hkv, G, 128)[heads].reshape(1, -1, 128), ref, f"{bits} G {G} slot {row}", tight=True)
+        assert (run([1], 1429) == 0).all() and (run([-1], 1429) == 7).all() and torch.isnan(run([2], 1428)).all()
 
 
 def test_attention_says_nan_where_it_cannot_know():
