@@ -604,8 +604,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     jh = (int)blockIdx.x; at_blk = 0;
     if (a.head_blocks > 1) { jh = (int)blockIdx.x / a.head_blocks; at_blk = (int)blockIdx.x - jh * a.head_blocks; }
     float workgroups = 0.0f;
-    constexpr bool kOneRow = NW == 12;      // (the form of 12 waves is for one long context)
-    if (kOneRow || n_rows == 1) {
+    if (n_rows == 1) {
       // One sequence: shares of the size that suits max_len (the host's), so that the page ids and the length are on their way together
       // (as a piece of a batch one small layer takes 7.6 us, 6.6 this way, 8 units x 2048 tokens 8.2 and 7.1).
       const int slot = rows ? load_uniform(rows) : 0;
@@ -625,11 +624,12 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
       a.items_q = a.share; a.items_r = 0; a.win_tiles = 0;
       part_row = (size_t)jh * a.n_splits;
       workgroups = (float)a.n_splits * a.groups;
-    } else if constexpr (!kOneRow) {
+    } else {
       __shared__ Piece s_piece;
       if (wave == 0) {
-        const Piece p = n_rows <= kWave ? find_piece<1>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
-                                        : find_piece<kBatchRows / kWave>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane);
+        // (12 waves: batches of a few rows only)
+        const Piece p = NW == 12 || n_rows <= kWave ? find_piece<1>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
+                                                    : find_piece<kBatchRows / kWave>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane);
         if (lane == 0) s_piece = p;
       }
       lds_barrier();
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
   if constexpr (PAGED) {
     if (last > tiles) last = tiles;                // (the last share of one sequence)
     ids_at = first;
-    if (NW != 12 && (items[3] & 1023u) != 1u) ids = load_ids();
+    if ((items[3] & 1023u) != 1u) ids = load_ids();
   }
 
   // ---- the query and the wave's first tile are requested before anything else is done.

@@ -84,6 +84,13 @@ PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits)
     if (p.waves == 12) p.block = G;
     p.share = tiles > splits ? (tiles + splits - 1) / splits : 1;
     p.pieces = tiles > 0 ? (tiles + p.share - 1) / p.share : 1;
+  } else if (G <= 8 && (long long)sh->B * sh->Hkv <= (G == 8 && v_bits >= 3 ? 64 : 32) && (long long)sh->B * sh->Hkv * tiles > 31 * kCus) {
+    // A few long contexts: one workgroup of 12 waves to a compute unit here too (2 x 8 units of 4 heads, 32k tokens 19.5 -> 18.1 us, of 32k and 32
+    // tokens at 3/4 bit 18.3 -> 16.7, 4 x 8 of 512 to 32k 19.0 -> 18.2, 4 x 8 of 8 heads, 16k 22.5 -> 19.9, 8 x 8 of 8 heads with 4-bit Values,
+    // 512 to 16k 25.0 -> 20.7). Not with more of them or shorter ones: 8 x 8 of 512 to 32k 22.1 and 25.3, 4 x 8 of 8k 13.2 both, 2 x 8 of 8k 11.1
+    // and 11.9, 2 x 32 of 1 head, 8k 15.6 and 16.1.
+    p.waves = 12;
+    p.block = G;
   }
   return p;
 }
@@ -267,7 +274,8 @@ int kvmix_paged_decode_attn(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, c
   a.head_blocks = plan.head_blocks;
   a.n_slots = p->n_slots; a.n_pages = p->n_pages; a.Hkv = sh->Hkv; a.window = p->window; a.max_len = max_len;
   a.groups = (float)(sh->Hkv * plan.head_blocks);
-  a.places = (float)kPlaces; a.inv_places = 1.0f / (float)kPlaces;
+  const int at_once = plan.waves == 12 ? kCus : kPlaces;
+  a.places = (float)at_once; a.inv_places = 1.0f / (float)at_once;
   a.share = plan.share; a.inv_share = 1.0f / (float)plan.share;
   a.ring_magic = ring_magic(a.ring_tiles);
   const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)kD);

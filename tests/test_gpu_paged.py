@@ -202,6 +202,15 @@ def test_one_sequence_in_workgroups_of_twelve_waves(bits):
         assert (run([1], 1429) == 0).all() and (run([-1], 1429) == 7).all() and torch.isnan(run([2], 1428)).all()
 
 
+@pytest.mark.parametrize("G,bits", [(1, (2, 2)), (2, (3, 3)), (4, (3, 4)), (8, (2, 4)), (8, (4, 1)), (16, (2, 2))])
+def test_a_few_long_sequences(G, bits):
+    """Four rows whose tiles are many for their few units: workgroups of 12 waves (8 with 16 heads), pieces of every row."""
+    s = Serving(2, G, bits, 32, n_slots=5, n_pages=2500, max_tiles=1300, seed=30 + G)
+    s.step([4, 0, 2, 1], [32 * 1200 + 50, 45, 32 * 700 + 33, 3000])
+    s.check_attention([2, 4, 1, 0], f"G {G}", max_len=32 * 1200 + 50)
+    s.check_attention([4, -1, 3, 4], f"G {G}, one twice", max_len=32 * 1200 + 50)
+
+
 def test_attention_says_nan_where_it_cannot_know():
     """A page id out of range, a length past max_len, below zero or past the table: NaN for that row, the others as ever."""
     import torch
