@@ -308,7 +308,7 @@ enum {                       /* bits of kvmix_pages.status */
   KVMIX_PAGES_EXHAUSTED = 1, /* kvmix_pages_grow: too few free pages, or more tiles than a table row holds: the row keeps its length */
   KVMIX_PAGES_BAD_ROW = 2,   /* a slot out of range, the same one twice, a length or an offset that cannot be */
   KVMIX_PAGES_BAD_ID = 4,    /* a page id out of range in the table or in a list of copies */
-  KVMIX_PAGES_OCCUPIED = 8   /* kvmix_pages_fork: the destination holds tokens, or is a source or a destination of the same call already */
+  KVMIX_PAGES_OCCUPIED = 8   /* kvmix_pages_fork: the destination holds tokens, or a slot is a source and a destination, or two destinations, of the call */
 };
 
 typedef struct {             /* every pointer: device memory, 4-byte aligned (moves: 16) */
@@ -322,7 +322,7 @@ typedef struct {             /* every pointer: device memory, 4-byte aligned (mo
                                 destinations; scratch */
   int32_t n_slots, n_pages;
   int32_t max_tiles;         /* entries of a table row */
-  int32_t window;            /* kvmix_layer_cfg.window of every layer, >= 0 */
+  int32_t window;            /* kvmix_layer_cfg.window of every layer, 0 to 2^30 */
 } kvmix_pages;
 
 typedef struct {             /* one layer's buffers (device, 16-byte aligned) */
@@ -340,8 +340,8 @@ int kvmix_pages_grow(const kvmix_pages* pages, const int32_t* rows, const int32_
 /* Slots are emptied: their pages' counts go down, pages that nobody holds are free. A slot named twice is freed once. */
 int kvmix_pages_free(const kvmix_pages* pages, const int32_t* rows, int n_rows, void* stream);
 /* Slot dst[i] (empty) becomes a second holder of the pages of slot src[i] and gets its length; the rings' rows are copied per layer by
- * kvmix_copy_windows. One source may have many destinations; a pair whose destination holds tokens, is named twice or is a source
- * of the same call is left out and sets a status bit. Negative slots: padding. At most 4096 pairs. */
+ * kvmix_copy_windows. One source may have many destinations; a pair whose destination holds tokens, is a destination
+ * twice or a source of the same call, or whose source is a destination of it, is left out and sets a status bit. Negative slots: padding. At most 4096 pairs. */
 int kvmix_pages_fork(const kvmix_pages* pages, const int32_t* src, const int32_t* dst, int n_pairs, void* stream);
 /* Pages in use move to the ids [0, in use): the i-th highest-numbered in use past that end (in ascending order) to the i-th free id below
  * it. Table, counts and bits are rewritten; moves holds the list for kvmix_move_records, which every layer's pool needs before it is
@@ -409,7 +409,7 @@ typedef struct {
 } kvmix_rope;                /* host memory; every device pointer 16-byte aligned */
 /* Queries and Keys of n_tokens tokens as the projections leave them, normed and rotated by positions[i], and Values, as the fp16 that the cache
  * and the attention take. Inputs of one type (kvmix_dtype). Angles are taken in binary64, everything else in fp32 with one rounding
- * at the end (|x| < 10^18 with a norm: the sum of squares is an fp32 number); positions (4-byte aligned) are any int32. An output may be its input's
+ * at the end (|x| < 10^18 with a norm: the sum of squares is an fp32 number; results past fp16 are infinite); fewer than 2^24 tokens; positions (4-byte aligned) are any int32. An output may be its input's
  * memory where the layout is the same, element for element. One launch. */
 int kvmix_qk_norm_rope(const kvmix_shape* shape, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions, void* stream);
 

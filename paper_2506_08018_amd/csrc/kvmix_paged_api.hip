@@ -7,6 +7,9 @@ using namespace kvmix;
 
 namespace {
 
+constexpr int kMostWorkgroups = 1 << 24;  // of 256 threads along one axis: threads are counted in 32 bits
+constexpr int kMostWindow = 1 << 30;      // (with what the largest table holds, lengths stay below 2^31)
+
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int check_pages(const kvmix_pages* p) {
@@ -14,7 +17,7 @@ int check_pages(const kvmix_pages* p) {
   if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->grown) || !aligned4(p->refs) || !aligned4(p->used) || !aligned4(p->status)) return KVMIX_ERR_ALIGN;
   // (fewer than 4 M pages: sums over the workgroup of the grow kernel fit 32 bits)
   if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages >= (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 23)) return KVMIX_ERR_BAD_SHAPE;
-  if (p->window < 0 || p->window % kTile) return KVMIX_ERR_BAD_SHAPE;
+  if (p->window < 0 || p->window > kMostWindow || p->window % kTile) return KVMIX_ERR_BAD_SHAPE;
   return KVMIX_OK;
 }
 
@@ -22,7 +25,7 @@ int check_paged_cfg(const kvmix_shape* sh, const kvmix_layer_cfg* cfg) {
   const int st = check_shape_cfg(sh, cfg);
   if (st) return st;
   if (cfg->k_bits == 16) return KVMIX_ERR_BAD_BITS;
-  return cfg->window < 0 ? KVMIX_ERR_BAD_SHAPE : KVMIX_OK;
+  return cfg->window < 0 || cfg->window > kMostWindow ? KVMIX_ERR_BAD_SHAPE : KVMIX_OK;
 }
 
 // `pool`, `rings`: what the call touches
@@ -184,8 +187,8 @@ int kvmix_copy_windows(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const 
 }
 
 int kvmix_paged_append(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const uint16_t* k_new, int64_t k_token_stride, int64_t k_head_stride,
-                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride, int n_tokens, const kvmix_paged_cache* c, const kvmix_pages* p, const int32_t* rows, const int32_t* cu, int max_new,
-                       void* stream) {
+                       const uint16_t* v_new, int64_t v_token_stride, int64_t v_head_stride, int n_tokens, const kvmix_paged_cache* c,
+                       const kvmix_pages* p, const int32_t* rows, const int32_t* cu, int max_new, void* stream) {
   int st = check_paged_cfg(sh, cfg);
   if (st) return st;
   st = check_paged_cache(cfg, c, true, true);
@@ -217,7 +220,7 @@ int kvmix_paged_append(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, const 
   a.more = 1 + (max_new <= kTile && a.ring_tiles > 2 ? 2 : a.ring_tiles);
   a.head_magic = ring_magic(sh->Hkv);
   const long long tiles = (long long)n_tokens / kTile + (long long)sh->B * a.more + 1;
-  if (tiles * sh->Hkv * sh->Hkv >= (1LL << 32) || tiles > 0x7fffffffLL) return KVMIX_ERR_BAD_SHAPE;
+  if (tiles * sh->Hkv * sh->Hkv >= (1LL << 32) || (tiles + 7) * sh->Hkv >= kMostWorkgroups) return KVMIX_ERR_BAD_SHAPE;
   const hipError_t e = launch_paged_append(a, cfg->k_bits, cfg->v_bits, (hipStream_t)stream);
   return e == hipSuccess ? KVMIX_OK : hip_fail(e);
 }
@@ -231,7 +234,7 @@ int kvmix_paged_workspace_bytes(const kvmix_shape* sh, int max_len, size_t* byte
   // (any window and any widths: a token counts for more in a window than in a page, so that one which holds everything has the most pieces)
   *bytes = 0;
   for (int v_bits = 2; v_bits <= 3; v_bits++) {
-    const PagedPlan p = plan_paged(sh, max_len / kTile * kTile, max_len, v_bits);
+    const PagedPlan p = plan_paged(sh, max_len < kMostWindow ? max_len / kTile * kTile : kMostWindow, max_len, v_bits);
     if (p.bytes > *bytes) *bytes = p.bytes;
   }
   return KVMIX_OK;
@@ -280,11 +283,18 @@ int kvmix_paged_decode_attn(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, c
   a.ring_magic = ring_magic(a.ring_tiles);
   const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)kD);
   a.scale_log2 = scale * 1.4426950408889634f;
-  for (int b = 0; b < sh->B; b += kRows) {
-    const int n = sh->B - b < kRows ? sh->B - b : kRows;
+  // (rows dealt out evenly: a launch of one row is another kind)
+  const int launches = (sh->B + kRows - 1) / kRows;
+  for (int i = 0, b = 0, n; i < launches; i++, b += n) {
+    n = sh->B / launches + (i < sh->B % launches ? 1 : 0);
     a.q = q + (size_t)b * sh->Hq * kD; a.out = out + (size_t)b * sh->Hq * kD;
     kvmix_pages here = *p;
-    if (!rows) { here.table += (size_t)b * p->max_tiles; here.lens += b; a.k_win = c->k_win + (size_t)b * sh->Hkv * c->W_cap * kD; a.v_win = c->v_win + (size_t)b * sh->Hkv * c->W_cap * kD; a.n_slots = p->n_slots - b; }
+    if (!rows) {      // (the launch's rows are slots from 0 on)
+      const size_t ring = (size_t)b * sh->Hkv * c->W_cap * kD;
+      here.table += (size_t)b * p->max_tiles; here.lens += b;
+      a.k_win = c->k_win + ring; a.v_win = c->v_win + ring;
+      a.n_slots = p->n_slots - b;
+    }
     const auto run = plan.waves == 12 ? launch_paged_attn<12> : launch_paged_attn<8>;
     const hipError_t e = run(a, here, rows ? rows + b : nullptr, n, plan.pieces, cfg->k_bits, cfg->v_bits, plan.block, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e);
@@ -325,7 +335,7 @@ int kvmix_qk_norm_rope(const kvmix_shape* sh, const kvmix_rope* rope, int dtype,
   if (!rope) return KVMIX_ERR_NULL;
   if (dtype != KVMIX_F16 && dtype != KVMIX_BF16 && dtype != KVMIX_F32) return KVMIX_ERR_BAD_SHAPE;
   if (rope->rotary_dim < 0 || rope->rotary_dim > kD || rope->rotary_dim % 16 || n_tokens < 0) return KVMIX_ERR_BAD_SHAPE;
-  if (!(rope->eps >= 0.0f)) return KVMIX_ERR_BAD_SHAPE;
+  if (!(rope->eps >= 0.0f) || n_tokens >= kMostWorkgroups) return KVMIX_ERR_BAD_SHAPE;
   if (rope->rotary_dim > 0 && !rope->frequencies) return KVMIX_ERR_NULL;
   if (!aligned16(rope->frequencies) || !aligned16(rope->q_weight) || !aligned16(rope->k_weight) || !aligned4(positions)) return KVMIX_ERR_ALIGN;
   const int step = dtype == KVMIX_F32 ? 4 : 8;       // elements of 16 bytes

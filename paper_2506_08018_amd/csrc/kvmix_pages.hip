@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kGrowThreads) void pages_grow_kernel(kvmix_pages p,
 #pragma unroll
   for (int e = 0; e < EACH; e++) {
     need[e] = 0; tiles[e] = 0;
-    if (ok[e] && (len[e] < 0 || fresh[e] < 0 || fresh[e] > 0x7fffffff - len[e])) { ok[e] = false; status |= KVMIX_PAGES_BAD_ROW; }
+    if (ok[e] && (len[e] < 0 || fresh[e] < 0 || fresh[e] > 0x7fffffff - len[e])) { ok[e] = false; status |= KVMIX_PAGES_BAD_ROW; p.grown[row[e]] = 0; }
     if (ok[e]) {
       tiles[e] = packed_tiles(len[e], p.window);
       const int after = packed_tiles(len[e] + fresh[e], p.window);
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kRowThreads) void pages_rename_kernel(kvmix_pages p
 // pieces of 16 KB for 4096 workgroups; rings of 32 slots x 8 heads, 50 MB read and written, 7.5 and 7.7.)
 constexpr int kPiece = 8192;
 __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a) {
-  const int n = a.count ? *a.count : a.n;
+  const int n = a.count && *a.count < a.n ? *a.count : a.n;      // (a.n: the most there can be)
   const uint32_t pieces = (uint32_t)((a.bytes + kPiece - 1) / kPiece), each = pieces * (uint32_t)a.n_base;
   const uint64_t total = (uint64_t)(n > 0 ? n : 0) * each;
   for (uint64_t at = blockIdx.x; at < total; at += gridDim.x) {

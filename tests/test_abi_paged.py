@@ -102,6 +102,22 @@ def test_counts_and_pointers(kv):
     assert attn(rows=None, sh=kv.Shape(9, 36, 4)) == -4                                # more batch rows than slots
 
 
+def test_sizes_past_what_is_counted_in_32_bits(kv):
+    """Windows whose lengths would not fit, more workgroups than a launch has."""
+    L, sh, r, a, W = kv.lib(), kv.Shape(2, 8, 4), C.byref, C.c_void_p(A), 2 ** 31 - 32
+    assert L.kvmix_pages_grow(r(pages(window=W)), a, a, 2, None) == L.kvmix_pages_compact(r(pages(window=2 ** 30 + 32)), None) == -4
+    cfg, c = kv.LayerCfg(2, 2, W), cache(W_cap=2 ** 31 - 32)
+    assert L.kvmix_copy_windows(r(sh), r(cfg), r(c), a, a, 2, None) == -4
+    assert L.kvmix_paged_append(r(sh), r(cfg), a, 512, 128, a, 512, 128, 9, r(c), r(pages(window=W)), a, a, 1, None) == -4
+    assert L.kvmix_paged_decode_attn(r(sh), r(cfg), a, r(c), r(pages(window=W)), a, 100, C.c_float(0), a, a, 1 << 30, None) == -4
+    cfg, c = kv.LayerCfg(2, 2, 64), cache()
+    assert L.kvmix_paged_append(r(sh), r(cfg), a, 0, 0, a, 0, 0, 2 ** 27, r(c), r(pages()), a, a, 2 ** 27, None) == -4
+    from paper_2506_08018_amd.binding import _rope_struct
+    rope = _rope_struct(A, 64, 0, 1.0, 1e-6, 0, 0, A, A, 0, 0, *[0] * 8)
+    assert L.kvmix_qk_norm_rope(r(sh), rope, 0, 2 ** 24, a, None) == -4
+    assert kv.paged_workspace_bytes(sh, 2 ** 31 - 1) >= kv.paged_workspace_bytes(sh, 2 ** 30) > 0
+
+
 @pytest.fixture(scope="module")
 def plan(tmp_path_factory):
     """kvmix_paged_decode_attn with its launch taken down: (B, Hkv, G, v_bits, W, max_len, workspace) -> status and, of the last

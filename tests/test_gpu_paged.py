@@ -211,6 +211,88 @@ def test_a_few_long_sequences(G, bits):
     s.check_attention([4, -1, 3, 4], f"G {G}, one twice", max_len=32 * 1200 + 50)
 
 
+@pytest.mark.parametrize("B,G,bits", [(64, 1, (2, 2)), (65, 4, (2, 3)), (300, 2, (1, 2)), (512, 1, (3, 2)), (513, 4, (2, 2)), (1300, 1, (4, 1))])
+def test_batches_of_many_rows(B, G, bits):
+    """More rows than a lane has one of, and more than a launch has: short contexts, empty ones and a few long ones; with the rows named and without."""
+    import torch
+    s = Serving(1, G, bits, 32, n_slots=B + 1, n_pages=9 * B, max_tiles=130, seed=B)
+    rows = [int(r) for r in s.rng.permutation(B + 1)[:B]]
+    fresh = [int(n) for n in s.rng.integers(0, 130, B)]
+    for b in (0, B // 2, B - 1):
+        fresh[b] = 3000 + b % 100
+    s.step(rows, fresh)
+    rows[1] = -1
+    looked_at = sorted({0, 2, B // 2 - 1, B // 2, B - 2, B - 1, *range(5, B, B // 25)})
+    ws = torch.zeros(s.kv.paged_workspace_bytes(s.shape(B), 130 * 32 + 63), dtype=torch.uint8, device="cuda")
+    for named in (rows, None, rows):
+        q = s.rng.standard_normal((B, G, 128), dtype=np.float32).astype(np.float16)
+        out = torch.full((B, G, 128), 7.0, dtype=torch.float16, device="cuda")
+        s.kv.paged_decode_attn(s.shape(B), s.cfg, torch.from_numpy(q).cuda(), s.cache, s.pages, out, ws, rows=None if named is None else s.ints(named))
+        got = t16(out)
+        for b in looked_at:
+            slot = b if named is None else named[b]
+            if s.ref.lens[slot] == 0:
+                assert (got[b] == 0).all()
+                continue
+            st, want = one_sequence(s.k[slot], s.v[slot], s.kb, s.vb, s.W, G).decode_attn(q[b:b + 1].view(np.uint16))
+            assert st == 0
+            assert_attn_close(got[b:b + 1], want, f"row {b} slot {slot} of {s.ref.lens[slot]} tokens, named {named is not None}", tight=True)
+        if named is not None:
+            assert (got[1].view(np.float16) == 7.0).all()
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 16 GB (2^32 words), rings of more than 4 GB, a table of more than 2^31 entries: what lies at their ends."""
+    import torch
+    import paper_2506_08018_amd as kv
+    Hkv, G, W, n_slots, n_pages = 8, 2, 32, 34000, 720000
+    shape, cfg, rng = kv.Shape(2, G * Hkv, Hkv), kv.LayerCfg(2, 2, W), np.random.default_rng(3)
+    pages = kv.Pages(n_slots, n_pages, 65000, W)
+    cache = kv.PagedCache(shape, cfg, n_pages, n_slots, 64)
+    assert cache.pool.numel() > 2 ** 32 and cache.k_win.numel() * 2 > 2 ** 32 and pages.table.numel() > 2 ** 31
+    pages.used[:-4] = -1                                    # the last 128 pages are free
+    pages.refs[:n_pages - 128] = 1
+    rows, fresh = [n_slots - 1, n_slots - 2], [2000, 700]
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    data = [[rng.standard_normal((Hkv, n, 128), dtype=np.float32).astype(np.float16) for _ in "kv"] for n in fresh]
+    k, v = (torch.from_numpy(np.concatenate([d[i] for d in data], 1)).cuda().transpose(0, 1) for i in (0, 1))
+    cu = ints([0, 2000, 2700])
+    kv.pages_grow(pages, ints(rows), cu)
+    kv.paged_append(shape, cfg, k, v, cache, pages, rows=ints(rows), cu=cu, max_new=2000)
+    q = rng.standard_normal((2, G * Hkv, 128), dtype=np.float32).astype(np.float16)
+    refs = [one_sequence(d[0], d[1], 2, 2, W, G) for d in data]
+
+    def look(rows, first_page, what):
+        at = first_page
+        for slot, rc, n in zip(rows, refs, fresh):
+            T = tiles_of(n, W)
+            ids = pages.table[slot, :T]
+            assert ids.tolist() == list(range(at, at + T)), what
+            at += T
+            assert np.array_equal(cache.pool[ids.long()].cpu().numpy().view(np.uint32), rc.packed[:, :T].transpose(1, 0, 2)), (what, slot)
+        out = torch.zeros((2, G * Hkv, 128), dtype=torch.float16, device="cuda")
+        ws = torch.zeros(kv.paged_workspace_bytes(shape, 2100), dtype=torch.uint8, device="cuda")
+        kv.paged_decode_attn(shape, cfg, torch.from_numpy(q).cuda(), cache, pages, out, ws, rows=ints(rows), max_len=2100)
+        for b, rc in enumerate(refs):
+            st, want = rc.decode_attn(q[b:b + 1].view(np.uint16))
+            assert st == 0
+            assert_attn_close(t16(out[b:b + 1]), want, f"{what} row {b}", tight=True)
+
+    look(rows, n_pages - 128, "at the ends")
+    pages.used[:-4] = 0
+    pages.refs[:n_pages - 128] = 0
+    kv.pages_fork(pages, ints(rows), ints([n_slots - 5, 1]))
+    kv.copy_windows(shape, cfg, cache, ints(rows), ints([n_slots - 5, 1]))
+    kv.pages_compact(pages)
+    kv.move_records(shape, cfg, cache, pages)
+    look([n_slots - 5, 1], 0, "forked and moved to the front")
+    look(rows, 0, "the first ones")
+    kv.pages_free(pages, ints([n_slots - 5, 1, *rows]))
+    assert not pages.refs.any() and not pages.used.any() and int(pages.status[0]) == 0
+    del pages, cache
+    torch.cuda.empty_cache()
+
+
 def test_attention_says_nan_where_it_cannot_know():
     """A page id out of range, a length past max_len, below zero or past the table: NaN for that row, the others as ever."""
     import torch

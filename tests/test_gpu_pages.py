@@ -81,6 +81,14 @@ def test_grow_refuses_bad_rows():
     assert s.pages.lens.cpu().tolist() == [0, 50, 70, 0]
 
 
+def test_grow_grants_nothing_where_a_count_cannot_be():
+    s = bare(4, 20, 9, 32)
+    s.grow([0, 1, 2], [50, 60, 70])
+    s.kv.pages_grow(s.pages, s.ints([0, 2, 1]), s.ints([10, 4, 2 ** 31 - 1, 2 ** 31 - 1]))      # fewer than no tokens; more than a length holds; none
+    assert s.pages.grown.cpu().tolist() == [0, 0, 0, 0] and s.pages.lens.cpu().tolist() == [50, 60, 70, 0]
+    assert int(s.pages.status[0]) == BAD_ROW
+
+
 def test_grow_without_rows_or_counts():
     s = bare(5, 20, 9, 0)
     for _ in range(33):
@@ -178,3 +186,14 @@ def test_copies(Hkv, bits, W):
     assert int(pages.moves[0]) == 0
     kv.move_records(shape, cfg, cache, pages)
     assert torch.equal(cache.pool, want)
+
+
+def test_moves_that_no_compaction_wrote():
+    """A list whose count is more than there can be, of ids that no pool has: nothing is moved, and status says so."""
+    s = Serving(2, 1, (2, 2), 32, 3, 10, 4, seed=8)
+    s.kv.pages_compact(s.pages)
+    s.pages.moves.fill_(-1)
+    s.pages.moves[0] = 2 ** 31 - 1
+    before = s.cache.pool.clone()
+    s.kv.move_records(s.shape(1), s.cfg, s.cache, s.pages)
+    assert bool((s.cache.pool == before).all()) and int(s.pages.status[0]) == BAD_ID
