@@ -312,7 +312,7 @@ enum {                       /* bits of kvmix_pages.status */
 };
 
 typedef struct {             /* every pointer: device memory, 4-byte aligned (moves: 16) */
-  int32_t* table;            /* [n_slots][max_tiles] page ids; entries past a sequence's tiles are not read */
+  int32_t* table;            /* [n_slots][max_tiles] page ids; entries past a sequence's tiles may hold anything */
   int32_t* lens;             /* [n_slots] tokens, those of the step in hand among them once kvmix_pages_grow has run */
   int32_t* grown;            /* [n_slots] tokens granted by the last kvmix_pages_grow (0 after a fork or free): what kvmix_paged_append takes */
   int32_t* refs;             /* [n_pages] slots that hold the page */
