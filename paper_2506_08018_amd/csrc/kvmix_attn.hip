@@ -381,7 +381,8 @@ template <int G> struct __attribute__((aligned(16))) WaveLds {
 
 // ---- PAGED: which piece of which context is a workgroup's, worked out by one of its waves from the lengths of the whole batch, which only
 // the device knows: a lane holds those of up to kBatchRows / 64 sequences. Pieces are tiles of a context, window tiles counted kWindowTiles each, a
-// context's all of one size and none larger than the share. The share is the best of four by a model of the launch (model_time). Shares of a size
+// context's all of one size and none larger than the share. The share is the best of four by a model of the launch (model_time), of those whose pieces
+// the grid has (plan_paged). Shares of a size
 // that the host takes from the longest length leave either long contexts in few workgroups or short ones in many, and a workgroup for every
 // piece that a shorter context does not have: 17 x 8 units of 64 to 8192 tokens took 27.7, 20.8, 17.2, 21.5 and 34.3 us in shares of 8, 16,
 // 32, 64 and 128 tiles (15.5 this way), 512 units of 2048 to 4096 tokens 92, 68.8, 54.5, 49.6 and 43.6 (43), 256 units of 64 to 32 768
@@ -468,7 +469,7 @@ __device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* 
     const float splits = c == 3 ? 1.0f : __builtin_ceilf(most * inv[c < 3 ? c : 0]);
     const float merge = splits > 1.0f ? kMergeTiles * splits : 0.0f;
     const float time = merge + model_time(workgroups, largest, fair, a.places, a.inv_places);
-    if (time < best) { best = time; choice = c; }
+    if (time < best && (c == 3 || (total >> (10 * c) & 1023) <= a.most_pieces)) { best = time; choice = c; }
   }
   choice = __builtin_amdgcn_readfirstlane(choice);
   Piece p = {};

@@ -175,6 +175,7 @@ __host__ __device__ __forceinline__ float model_time(float workgroups, float lar
 constexpr float kShares[3] = {1.1f, 1.5f, 2.2f};      // shares of a batch that are tried, besides whole contexts: times what each of `places` would get
 struct PagedAttnArgs : AttnArgs {
   int n_slots, n_pages, Hkv, window, max_len;
+  int most_pieces;        // that the grid has workgroups for
   float groups;           // workgroups of a piece: kv heads x blocks of heads
   float places, inv_places;      // workgroups that the chip holds at once
   int share;              // one sequence: tiles of a workgroup, by max_len

@@ -47,8 +47,10 @@ uint32_t ring_magic(int ring_tiles) { return ring_tiles == 1 ? 0u : (uint32_t)((
 
 // A ragged launch: batch rows in launches of at most kRows, each with a workgroup per piece of a context, kv head and block of heads.
 // Pieces are made on the device (find_piece in kvmix_attn.hip): from the tiles of the whole batch a share for each of the kPlaces
-// workgroups that the chip holds at once (8 waves, two to a compute unit), so that there are at most kPlaces / (kv heads x head blocks)
-// pieces and one more for every row.
+// workgroups that the chip holds at once (8 waves, two to a compute unit), or somewhat more. The grid has as many pieces as the chip holds while the rows
+// are no more than half of that: in shares of 2.2 (kShares) they always fit. For more rows it has the rows and what shares of 2.2 cut off besides: where
+// workgroups queue, few large pieces are better (48 x 8 units of 4 heads, 512 to 8192 tokens 35.4 -> 32.9 us, 64 x 8 of 1 to 4096 20.4 -> 18.6 against a
+// grid for every piece that shares of 1.1 make), and each workgroup that finds no piece takes 2 us at the end.
 constexpr int kRows = 512, kCus = 256, kPlaces = 2 * kCus;
 constexpr float kAloneInTwelve = 0.55f;       // kAlone of a workgroup of 12 waves
 struct PagedPlan { int block, head_blocks, rows, pieces, share, waves; size_t counters, bytes; };
@@ -61,11 +63,21 @@ PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits)
   p.rows = sh->B < kRows ? sh->B : kRows;
   const int tiles = packed_tiles(max_len, window), held = max_len - window < kTile ? max_len : window + kTile - 1;
   const long long most = tiles + (long long)kWindowTiles * (((long long)held + kTile - 1) / kTile), each = most <= kMinShare ? 1 : (most + kMinShare - 1) / kMinShare;
-  const long long by_places = p.rows + kPlaces / (sh->Hkv * p.head_blocks) + 1, by_length = p.rows * each;
+  const bool few_long = sh->B > 1 && G <= 8 && (long long)sh->B * sh->Hkv <= (G == 8 && v_bits >= 3 ? 64 : 32) && (long long)sh->B * sh->Hkv * tiles > 31 * kCus;
+  p.share = 1; p.waves = 8;
+  if (few_long) {
+    // A few long contexts: one workgroup of 12 waves to a compute unit, as for one sequence (2 x 8 units of 4 heads, 32k tokens 19.5 -> 18.1 us, of 32k
+    // and 32 tokens at 3/4 bit 18.3 -> 16.7, 4 x 8 of 512 to 32k 19.0 -> 18.2, 4 x 8 of 8 heads, 16k 22.5 -> 19.9, 8 x 8 of 8 heads with 4-bit
+    // Values, 512 to 16k 25.0 -> 20.7). Not with more of them or shorter ones: 8 x 8 of 512 to 32k 21.5 and 25.3, 16 x 8 of 8k 25.4 and 28.4, 4 x 8
+    // of 8k 13.2 both, 2 x 8 of 8k 11.1 and 11.9, 4 x 32 of 1 head, 256 to 8k 16.4 and 17.5.
+    p.waves = 12;
+    p.block = G;
+  }
+  const int held_at_once = (p.waves == 12 ? kCus : kPlaces) / (sh->Hkv * p.head_blocks);
+  const long long by_places = p.rows <= held_at_once / 2 ? held_at_once : p.rows + held_at_once * 5 / 11 + 1, by_length = p.rows * each;
   p.pieces = (int)(by_places < by_length ? by_places : by_length);
   p.counters = ((size_t)p.rows * sh->Hkv * (G > 8 ? G / 8 : 1) * 4 + 255) / 256 * 256;
   p.bytes = p.counters + (size_t)p.pieces * sh->Hkv * G * (kD + 2) * sizeof(float);
-  p.share = 1; p.waves = 8;
   if (sh->B == 1) {
     // One sequence: unsplit, one workgroup or two to a compute unit, at most 64 pieces (1 x 8 heads over 32k tokens: 64 pieces 13.0 us, 256
     // 17.0), by the model of a batch's launch. One to a compute unit has 12 waves where there are more than 20 tiles for it: 8 x 4 heads over
@@ -87,13 +99,6 @@ PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits)
     if (p.waves == 12) p.block = G;
     p.share = tiles > splits ? (tiles + splits - 1) / splits : 1;
     p.pieces = tiles > 0 ? (tiles + p.share - 1) / p.share : 1;
-  } else if (G <= 8 && (long long)sh->B * sh->Hkv <= (G == 8 && v_bits >= 3 ? 64 : 32) && (long long)sh->B * sh->Hkv * tiles > 31 * kCus) {
-    // A few long contexts: one workgroup of 12 waves to a compute unit here too (2 x 8 units of 4 heads, 32k tokens 19.5 -> 18.1 us, of 32k and 32
-    // tokens at 3/4 bit 18.3 -> 16.7, 4 x 8 of 512 to 32k 19.0 -> 18.2, 4 x 8 of 8 heads, 16k 22.5 -> 19.9, 8 x 8 of 8 heads with 4-bit Values,
-    // 512 to 16k 25.0 -> 20.7). Not with more of them or shorter ones: 8 x 8 of 512 to 32k 22.1 and 25.3, 4 x 8 of 8k 13.2 both, 2 x 8 of 8k 11.1
-    // and 11.9, 2 x 32 of 1 head, 8k 15.6 and 16.1.
-    p.waves = 12;
-    p.block = G;
   }
   return p;
 }
@@ -233,8 +238,9 @@ int kvmix_paged_workspace_bytes(const kvmix_shape* sh, int max_len, size_t* byte
   if (max_len < 1) return KVMIX_ERR_BAD_SHAPE;
   // (any window and any widths: a token counts for more in a window than in a page, so that one which holds everything has the most pieces)
   *bytes = 0;
+  if (max_len > kMostWindow) max_len = kMostWindow;      // (long before that the pieces are as many as the chip holds)
   for (int v_bits = 2; v_bits <= 3; v_bits++) {
-    const PagedPlan p = plan_paged(sh, max_len < kMostWindow ? max_len / kTile * kTile : kMostWindow, max_len, v_bits);
+    const PagedPlan p = plan_paged(sh, max_len / kTile * kTile, max_len, v_bits);
     if (p.bytes > *bytes) *bytes = p.bytes;
   }
   return KVMIX_OK;
@@ -279,6 +285,7 @@ int kvmix_paged_decode_attn(const kvmix_shape* sh, const kvmix_layer_cfg* cfg, c
   a.groups = (float)(sh->Hkv * plan.head_blocks);
   const int at_once = plan.waves == 12 ? kCus : kPlaces;
   a.places = (float)at_once; a.inv_places = 1.0f / (float)at_once;
+  a.most_pieces = plan.pieces;
   a.share = plan.share; a.inv_share = 1.0f / (float)plan.share;
   a.ring_magic = ring_magic(a.ring_tiles);
   const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)kD);
