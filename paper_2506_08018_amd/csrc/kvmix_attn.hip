@@ -385,8 +385,8 @@ template <int G> struct __attribute__((aligned(16))) WaveLds {
 // the grid has (plan_paged). Shares of a size
 // that the host takes from the longest length leave either long contexts in few workgroups or short ones in many, and a workgroup for every
 // piece that a shorter context does not have: 17 x 8 units of 64 to 8192 tokens took 27.7, 20.8, 17.2, 21.5 and 34.3 us in shares of 8, 16,
-// 32, 64 and 128 tiles (15.5 this way), 512 units of 2048 to 4096 tokens 92, 68.8, 54.5, 49.6 and 43.6 (43), 256 units of 64 to 32 768
-// tokens 136, 86.7, 63, 52.6 and 49.9 (33). The price is 1.3 us at the start of every workgroup: the lengths' way from memory in front of the
+// 32, 64 and 128 tiles (15.1 this way), 512 units of 2048 to 4096 tokens 92, 68.8, 54.5, 49.6 and 43.6 (41.5), 256 units of 64 to 32 768
+// tokens 136, 86.7, 63, 52.6 and 49.9 (32). The price is 1.3 us at the start of every workgroup: the lengths' way from memory in front of the
 // page ids' and some 150 instructions of one wave (by every wave for itself, with seven shares tried one after the other, 1.9).
 constexpr int kBatchRows = 512;          // of one launch
 struct Piece { int row, slot, len, sp, splits, first, total, items_q, items_r, win_each, win_extra, win_tiles, n_w, tiles; };      // row -1: none; first: of the row's pieces
@@ -476,13 +476,16 @@ __device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* 
   p.row = -1;
   p.total = choice == 3 ? here : total >> (10 * choice) & 1023;
   if (k >= p.total) return p;
+  // Large pieces first, by eighths of the largest: what is dispatched last is small. Where all are resident, and some compute units
+  // have two, the small ones go with large ones: workgroups are placed unit after unit (as far as can be told), so that the k-th meets the
+  // (k + units)-th.
+  const float eighths = 8.0f * __builtin_amdgcn_rcpf(fmaxf(fminf(share[choice], most), 1.0f));
+  const int units_each = (int)(0.5f * a.places * __builtin_amdgcn_rcpf(groups)), second = p.total - units_each;
+  if (second > 0 && second <= units_each) k = k >= units_each ? p.total - 1 - (k - units_each) : k < second ? k + units_each - second : k - second;
+  auto pieces_of = [&](int r) { return choice == 3 ? (slot[r] >= 0 ? 1 : 0) : cuts[r] >> (10 * choice) & 1023; };
+  auto size_of = [&](int r, int n) { return n == 0 ? -1 : (int)fminf(units[r] * __builtin_amdgcn_rcpf((float)n) * eighths, 7.0f); };
   if constexpr (N == 1) {
-    // Large pieces first, by eighths of the largest: what is dispatched last is small. Where all are resident, and some compute units
-    // have two, the small ones go with large ones: workgroups are placed unit after unit (as far as can be told), so that the k-th meets the
-    // (k + units)-th.
-    const int n = choice == 3 ? (slot[0] >= 0 ? 1 : 0) : cuts[0] >> (10 * choice) & 1023;
-    const float eighths = 8.0f * __builtin_amdgcn_rcpf(fmaxf(fminf(share[choice], most), 1.0f));
-    const int size = n == 0 ? -1 : (int)fminf(units[0] * __builtin_amdgcn_rcpf((float)n) * eighths, 7.0f);
+    const int n = pieces_of(0), size = size_of(0, n);
     int rank = 0, ahead = 0;
 #pragma unroll
     for (int c = 7; c >= -1; c--) {
@@ -492,8 +495,6 @@ __device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* 
       ahead += __popcll(m);
     }
     const int sorted = __builtin_amdgcn_ds_permute(4 * rank, lane << 10 | n), up = wave_scan(sorted & 1023);
-    const int units_each = (int)(0.5f * a.places * __builtin_amdgcn_rcpf(groups)), second = p.total - units_each;
-    if (second > 0 && second <= units_each) k = k >= units_each ? p.total - 1 - (k - units_each) : k < second ? k + units_each - second : k - second;
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(k < up));
     const int picked = __builtin_amdgcn_readlane(sorted, at), l = picked >> 10;
     p.row = l;
@@ -501,27 +502,47 @@ __device__ __forceinline__ Piece find_piece(const int32_t* rows, const int32_t* 
     p.len = __builtin_amdgcn_readlane(len[0], l);
     p.splits = picked & 1023;
     p.first = __builtin_amdgcn_readlane(up, at) - p.splits;
-    p.sp = k - p.first;
-  }
-  int before = 0;
+  } else {
+    // Pieces of each size, 10 bits each in three sums (no more than 1023 together); then the rows of the size in which the k-th is. (As the rows
+    // come 100 x 8 units of 1 head, 64 to 4096 tokens take 35.4 us, 300 x 4 of 4 heads 56.3, 512 x 1 of 8 heads, 64 to 8192 47.1; this way 33.1, 47.2
+    // and 36.8.)
+    uint32_t in_size[3] = {0, 0, 0};
+    int n[N], size[N];
 #pragma unroll
-  for (int r = 0; r < (N == 1 ? 0 : N); r++) {
-    const uint64_t there = __builtin_amdgcn_ballot_w64(slot[r] >= 0);
-    const int n = choice == 3 ? (slot[r] >= 0 ? 1 : 0) : cuts[r] >> (10 * choice) & 1023;
-    const int up = choice == 3 ? before + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0)) + n
-                               : upto[r] >> (10 * choice) & 1023;
-    const uint64_t past = __builtin_amdgcn_ballot_w64(k < up);
-    if (p.row < 0 && past) {
-      const int l = __builtin_ctzll(past);
-      p.row = kWave * r + l;
-      p.slot = __builtin_amdgcn_readlane(slot[r], l);
-      p.len = __builtin_amdgcn_readlane(len[r], l);
-      p.splits = __builtin_amdgcn_readlane(n, l);
-      p.first = __builtin_amdgcn_readlane(up, l) - p.splits;
-      p.sp = k - p.first;
+    for (int r = 0; r < N; r++) {
+      n[r] = pieces_of(r);
+      size[r] = size_of(r, n[r]);
+      const uint32_t add = size[r] < 0 ? 0u : (uint32_t)n[r] << (10 * (size[r] % 3));
+#pragma unroll
+      for (int w = 0; w < 3; w++) in_size[w] += size[r] / 3 == w ? add : 0u;
     }
-    before += __popcll(there);
+#pragma unroll
+    for (int w = 0; w < 3; w++) in_size[w] = (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)in_size[w]), kWave - 1);
+    int c = 7, before = 0;
+    for (; c > 0; c--) {
+      const int all = (int)(in_size[2] >> 10 & 1023u);      // (of size 7 first: the sums move up by a size each time)
+      if (k < before + all) break;
+      before += all;
+      in_size[2] = in_size[2] << 10 | (in_size[1] >> 20 & 1023u);
+      in_size[1] = in_size[1] << 10 | (in_size[0] >> 20 & 1023u);
+      in_size[0] <<= 10;
+    }
+#pragma unroll
+    for (int r = 0; r < N; r++) {
+      const int mine = size[r] == c ? n[r] : 0, up = before + wave_scan(mine);
+      const uint64_t past = __builtin_amdgcn_ballot_w64(k < up);
+      if (p.row < 0 && past) {
+        const int l = __builtin_ctzll(past);
+        p.row = kWave * r + l;
+        p.slot = __builtin_amdgcn_readlane(slot[r], l);
+        p.len = __builtin_amdgcn_readlane(len[r], l);
+        p.splits = __builtin_amdgcn_readlane(n[r], l);
+        p.first = __builtin_amdgcn_readlane(up, l) - p.splits;
+      }
+      before = __builtin_amdgcn_readlane(up, kWave - 1);
+    }
   }
+  p.sp = k - p.first;
   // as plan_attention deals a context out
   const int n = p.len < 0 ? 0 : p.len;
   p.tiles = packed_tiles(n, a.window);
@@ -628,8 +649,11 @@ __global__ __launch_bounds__(NW * kWave, NW == 12 ? 3 : 4) void decode_attn_kern
     } else {
       __shared__ Piece s_piece;
       if (wave == 0) {
-        // (12 waves: batches of a few rows only)
+        // A lane has as few rows as will do (65 x 8 units of 4 heads 49.7 us with eight, 43.2 with two; 129 x 8 42.3 with eight, 39.3 with
+        // four). 12 waves: batches of a few rows only.
         const Piece p = NW == 12 || n_rows <= kWave ? find_piece<1>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
+                        : n_rows <= 2 * kWave       ? find_piece<2>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
+                        : n_rows <= 4 * kWave       ? find_piece<4>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane)
                                                     : find_piece<kBatchRows / kWave>(rows, lens, n_rows, n_ids, a, blockIdx.y, lane);
         if (lane == 0) s_piece = p;
       }
