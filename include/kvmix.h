@@ -358,7 +358,8 @@ int kvmix_copy_windows(const kvmix_shape* shape, const kvmix_layer_cfg* cfg, con
 /* kvmix_append_tokens for a ragged batch, after kvmix_pages_grow: the tokens [cu[b], cu[b + 1]) of k_new, v_new (element (i, j, d) of
  * each at i*token_stride + j*head_stride + d; strides of their own, in elements, multiples of 8, not negative; 16-byte aligned) are the newest of
  * slot rows[b], b < shape->B. Tiles that fall due are quantized into their pages exactly as in kvmix_quantize_pack, from the ring or
- * straight from the input; what stays goes into the ring; one launch. n_tokens: tokens of the inputs. max_new: no row brings more. A
+ * straight from the input; what stays goes into the ring; one launch. The rows are some of those of the last
+ * kvmix_pages_grow (another slot would still have the grown[s] of its own last one). n_tokens: tokens of the inputs. max_new: no row brings more. A
  * row whose token count is not what grown[s] says, exceeds max_new or goes past n_tokens is left alone. */
 int kvmix_paged_append(const kvmix_shape* shape, const kvmix_layer_cfg* cfg,
                        const uint16_t* k_new, int64_t k_token_stride, int64_t k_head_stride,

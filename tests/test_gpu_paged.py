@@ -241,6 +241,23 @@ def test_batches_of_many_rows(B, G, bits):
             assert (got[1].view(np.float16) == 7.0).all()
 
 
+@pytest.mark.parametrize("B,G", [(1, 4), (2, 8), (7, 1), (70, 2), (200, 16), (515, 1)])
+def test_batches_of_padding_and_of_empty_sequences(B, G):
+    """Nothing but padding: nothing is written, by any of the calls; nothing but empty sequences: zeros."""
+    import torch
+    s = Serving(2, G, (2, 3), 32, n_slots=B, n_pages=4, max_tiles=20, seed=B)
+    pool, ring = s.cache.pool.clone(), s.cache.k_win.clone()
+    s.grow([-1] * B, [40] * B)
+    s.append([-1] * B, [40] * B)
+    s.kv.paged_append(s.shape(B), s.cfg, *torch.zeros((2, B, 2, 128), dtype=torch.float16, device="cuda"), s.cache, s.pages, rows=s.ints([-1] * B))
+    s.check_attention([-1] * B, "padding")
+    s.grow(range(B), [0] * B)
+    s.append(range(B), [0] * B)
+    s.check_attention(list(range(B)), "empty")
+    s.check_pages()
+    assert torch.equal(s.cache.pool, pool) and torch.equal(s.cache.k_win.view(torch.int16), ring.view(torch.int16))
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 16 GB (2^32 words), rings of more than 4 GB, a table of more than 2^31 entries: what lies at their ends."""
     import torch
