@@ -410,8 +410,8 @@ typedef struct {
 } kvmix_rope;                /* host memory; every device pointer 16-byte aligned */
 /* Queries and Keys of n_tokens tokens as the projections leave them, normed and rotated by positions[i], and Values, as the fp16 that the cache
  * and the attention take. Inputs of one type (kvmix_dtype). Angles are taken in binary64, everything else in fp32 with one rounding
- * at the end (|x| < 10^18 with a norm: the sum of squares is an fp32 number; results past fp16 are infinite); fewer than 2^24 tokens; positions (4-byte aligned) are any int32. An output may be its input's
- * memory where the layout is the same, element for element. One launch. */
+ * at the end (|x| < 10^18 with a norm: the sum of squares is an fp32 number; results past fp16 are infinite). Fewer than 2^24 tokens;
+ * positions (4-byte aligned) are any int32. An output may be its input's memory where the layout is the same, element for element. One launch. */
 int kvmix_qk_norm_rope(const kvmix_shape* shape, const kvmix_rope* rope, int dtype, int n_tokens, const int32_t* positions, void* stream);
 
 #ifdef __cplusplus

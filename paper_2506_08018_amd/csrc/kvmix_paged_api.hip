@@ -14,7 +14,8 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 int check_pages(const kvmix_pages* p) {
   if (!p || !p->table || !p->lens || !p->grown || !p->refs || !p->used || !p->status) return KVMIX_ERR_NULL;
-  if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->grown) || !aligned4(p->refs) || !aligned4(p->used) || !aligned4(p->status)) return KVMIX_ERR_ALIGN;
+  if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->grown)) return KVMIX_ERR_ALIGN;
+  if (!aligned4(p->refs) || !aligned4(p->used) || !aligned4(p->status)) return KVMIX_ERR_ALIGN;
   // (fewer than 4 M pages: sums over the workgroup of the grow kernel fit 32 bits)
   if (p->n_slots < 1 || p->n_slots > (1 << 20) || p->n_pages < 1 || p->n_pages >= (1 << 22) || p->max_tiles < 1 || p->max_tiles > (1 << 23)) return KVMIX_ERR_BAD_SHAPE;
   if (p->window < 0 || p->window > kMostWindow || p->window % kTile) return KVMIX_ERR_BAD_SHAPE;
@@ -62,8 +63,10 @@ PagedPlan plan_paged(const kvmix_shape* sh, int window, int max_len, int v_bits)
   p.head_blocks = (G + p.block - 1) / p.block;
   p.rows = sh->B < kRows ? sh->B : kRows;
   const int tiles = packed_tiles(max_len, window), held = max_len - window < kTile ? max_len : window + kTile - 1;
-  const long long most = tiles + (long long)kWindowTiles * (((long long)held + kTile - 1) / kTile), each = most <= kMinShare ? 1 : (most + kMinShare - 1) / kMinShare;
-  const bool few_long = sh->B > 1 && G <= 8 && (long long)sh->B * sh->Hkv <= (G == 8 && v_bits >= 3 ? 64 : 32) && (long long)sh->B * sh->Hkv * tiles > 31 * kCus;
+  const long long most = tiles + (long long)kWindowTiles * (((long long)held + kTile - 1) / kTile);
+  const long long each = most <= kMinShare ? 1 : (most + kMinShare - 1) / kMinShare;
+  const long long units = (long long)sh->B * sh->Hkv;
+  const bool few_long = sh->B > 1 && G <= 8 && units <= (G == 8 && v_bits >= 3 ? 64 : 32) && units * tiles > 31 * kCus;
   p.share = 1; p.waves = 8;
   if (few_long) {
     // A few long contexts: one workgroup of 12 waves to a compute unit, as for one sequence (2 x 8 units of 4 heads, 32k tokens 19.5 -> 18.1 us, of 32k

@@ -258,6 +258,22 @@ def test_batches_of_padding_and_of_empty_sequences(B, G):
     assert torch.equal(s.cache.pool, pool) and torch.equal(s.cache.k_win.view(torch.int16), ring.view(torch.int16))
 
 
+@pytest.mark.parametrize("G", [1, 4, 8, 16])
+def test_one_workspace_for_layers_of_other_widths(G):
+    """Layers of one shape share a workspace that was zeroed once: other widths, bounds on the length that make other launches, results that are NaN."""
+    import torch
+    layers = [Serving(2, G, bits, 32, n_slots=4, n_pages=600, max_tiles=1300, seed=50 + G) for bits in ((2, 2), (3, 4), (1, 3))]
+    for s in layers:
+        s.step([1, 3, 0, 2], [5000, 40, 3000, 4500])
+    ws = torch.zeros(layers[0].kv.paged_workspace_bytes(layers[0].shape(4), 1300 * 32 + 63), dtype=torch.uint8, device="cuda")
+    for turn in range(3):
+        for s in layers:
+            for max_len in (0, 5000, 1300 * 32):
+                s.check_attention([0, 1, 2, 3], f"{s.kb}/{s.vb} {max_len} turn {turn}", max_len=max_len, ws=ws)
+            got, _ = s.attend([0, 1, 2, 3], max_len=4800, ws=ws)
+            assert np.isnan(got[1].view(np.float16)).all() and np.isfinite(got[[0, 2, 3]].view(np.float16)).all()
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 16 GB (2^32 words), rings of more than 4 GB, a table of more than 2^31 entries: what lies at their ends."""
     import torch
