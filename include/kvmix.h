@@ -298,7 +298,8 @@ int kvmix_stream_read(const void* buf, size_t bytes, int workgroups, int threads
  * layers, which then have one window length) and a kvmix_paged_cache for each layer. A step is
  *   kvmix_pages_grow(rows, cu)                                   once: lengths, pages for the tiles that fall due
  *   kvmix_qk_norm_rope, kvmix_paged_append, kvmix_paged_decode_attn   for each layer
- * `rows`: the slot of every batch row (NULL: row b is slot b); a negative one is padding, for which nothing is read or written. The
+ * `rows`: the slot of every batch row (NULL: row b is slot b); a negative one is padding, for which nothing is written (its
+ * token of an input may be read). The
  * slots of a batch are distinct where a call writes to them. `cu`: n_rows + 1 offsets, row b brings the tokens [cu[b], cu[b + 1]) of the
  * call's inputs (NULL: token b alone).
  * What the host cannot see is checked on the device: nothing is read or written outside the buffers whatever these integers
