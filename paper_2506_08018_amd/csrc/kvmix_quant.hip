@@ -723,7 +723,8 @@ __global__ __launch_bounds__(128, 4) void quantize_pack_many_kernel(QuantArgs a)
 // and their heads follow each other, so that a die has the rows of a token from all heads. (As many tiles for every row as the longest may have, most
 // of them without work: 7 rows of 1 to 8000 tokens 19.7 us, 15.6 now.) Without cu, single tokens: one workgroup for a row and head, which also
 // fills the ring behind a due tile (256 rows x 8 heads 6.9 us, 9.3 with a workgroup for either); the token's rows are asked for ahead of its slot and
-// length, and without a due tile stored as they come (1000 rows x 8 heads 17.0 -> 10.9 us, 256 6.9 -> 5.7, 1 row 2.4 -> 2.0).
+// length, and without a due tile stored as they come (8 heads, no tile due: 1000 rows 14.7 -> 8.3 us, 256 5.2 -> 3.5, 64 2.85 -> 2.33, one 2.4 -> 2.0; one row
+// in 32 with a due tile: 16.4 -> 11.0, 6.9 -> 5.55, 4.4 -> 4.3).
 // What is in front of a tile's first request, two ways to memory and some 100 instructions, is not hidden where the registers hold no more
 // workgroups: a prompt of 32 700 tokens takes 39.3 us at 3/4 bit and 35.2 at 2/2, the contiguous cache's 33.5 and 30.4. Several tiles to a
 // workgroup, one after the other, spill (59 us with two).
